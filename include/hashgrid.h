@@ -394,6 +394,77 @@ hg_status hashgrid_train_step(const hashgrid_t* hg, const hashgrid_train_state* 
                               const float* target, void* y, void* dLdy, void* workspace, uint64_t workspace_bytes,
                               uint32_t step, void* stream);
 
+/* Between the gradients and the optimiser: the norm over the gradients of all of a model's tensors (the tables, the network's weights,
+ * a caller's own), clipping by it, and the Adam step on all tensors with the gradients clipped on the way.  Nothing comes back
+ * to the host: what the norm decides stays in a hashgrid_grad_stats in device memory, where the later calls read it, so that a
+ * training loop does not wait and a whole step can be captured into a graph and replayed, the optimiser's step number included. */
+#define HG_BF16 2u                           /* beside HG_F32 and HG_F16, in the lists below only */
+#define HG_MAX_TENSORS 1024u                 /* tensors a call; more returns HG_ERR_UNSUPPORTED */
+#define HG_MAX_TENSOR_SCALARS (1ull << 42)   /* scalars a tensor; as all tensors of a call together */
+#define HG_GRAD_NORM_GROUPS 2048u
+
+typedef struct {
+  void* data;         /* device, aligned to its element; not looked at when n_scalars == 0 */
+  uint64_t n_scalars;
+  uint32_t dtype;     /* HG_F32, HG_F16 or HG_BF16 */
+  uint32_t reserved;  /* 0 */
+} hashgrid_grad;
+
+/* Device memory, 16-byte aligned, ALL ZERO before its first use; one per model.  Calls that overlap in time need one each. */
+typedef struct {
+  float norm;      /* of the last hashgrid_grad_norm; NaN or infinity where a gradient is */
+  float factor;    /* min(1, max_norm / norm); 0 where the sum of the squares is not finite */
+  uint32_t step;   /* number of the optimiser step that is due: steps + 1, or 0 where the sum is not finite: left out */
+  uint32_t steps;  /* optimiser steps taken (hashgrid_adam_steps).  A caller that resumes sets it. */
+  uint32_t scratch[4];
+  double partials[HG_GRAD_NORM_GROUPS]; /* scratch */
+} hashgrid_grad_stats;
+
+/* norm = grad_scale * sqrt(sum of the squares of all scalars of all tensors) and what follows from it, into *stats.
+ * Squares and sums are held in 64 bits: no gradient is too large or too small to count, and norm is within a unit in its last
+ * place of the exact one (infinity beyond fp32's range; factor does not suffer from that).  The same arrays give the same bits.
+ *   grads       [n_tensors]  HOST array, read during the call; data is read only
+ *   grad_scale  finite and positive: 1, or the reciprocal of the factor by which the loss was scaled
+ *   max_norm    >= 0, infinity: no clipping, the norm is only measured (and step set)
+ * A tensor that stands in the list twice counts twice.  n_tensors == 0, or tensors without scalars: the norm is 0, factor 1.
+ * HG_ERR_INVALID_ARG for NULL or misaligned pointers, an unknown dtype, scales out of range. */
+hg_status hashgrid_grad_norm(uint32_t n_tensors, const hashgrid_grad* grads, float grad_scale, float max_norm,
+                             hashgrid_grad_stats* stats, void* stream);
+
+/* out_i = factor * grads_i, each product rounded once to the tensor's type, with the factor that hashgrid_grad_norm has left in
+ * *stats: the gradients keep their loss scale.  factor == 0 (max_norm 0, or a gradient that is not finite) writes zeros, which
+ * hashgrid_adam_step passes over.
+ *   out  [n_tensors]  HOST array of device pointers to arrays of the gradients' types and sizes; out[i] == grads[i].data
+ *                     is in place.  NULL: all in place; where factor is 1 nothing is read or written then.
+ * HG_ERR_INVALID_ARG also where an array that is written shares memory with another one of the call. */
+hg_status hashgrid_clip_grads(uint32_t n_tensors, const hashgrid_grad* grads, void* const* out,
+                              const hashgrid_grad_stats* stats, void* stream);
+
+typedef struct {
+  float* params_master; /* [n] fp32, read and written (this and the other arrays: device, aligned to their element) */
+  void* params_half;    /* [n] half_dtype, may be NULL: the rounded (nearest even) master copy, before the call as after it */
+  void* grad;           /* [n] grad_dtype, read; set to 0 where it was not when zero_grad != 0 */
+  float* m;             /* [n] fp32, first and second moment, read and written */
+  float* v;
+  uint64_t n_scalars;   /* n; 0: the pointers are not looked at */
+  uint32_t grad_dtype;  /* HG_F32, HG_F16 or HG_BF16 */
+  uint32_t half_dtype;  /* HG_F16 or HG_BF16 */
+  hashgrid_adam_config cfg;
+  uint32_t reserved;    /* 0 */
+} hashgrid_adam_tensor;
+
+/* hashgrid_adam_step on every tensor of the list, in one launch for every three dozen of them.  The gradient that the step takes is
+ * grad * (grad_scale * factor), in fp32, plus cfg.l2_reg * value; scalars for which that is exactly 0 are passed over.
+ *   tensors  [n_tensors]  HOST array, read during the call
+ *   stats    NULL: factor 1, and the step's number is `step` >= 1.
+ *            Else `step` is 0 and both come from the last hashgrid_grad_norm on *stats: factor, and step, which becomes
+ *            stats->steps.  Where step is 0 (a gradient that is not finite, or no norm taken yet) nothing is updated, whatever l2_reg;
+ *            zero_grad still clears the gradients.  Several calls after one hashgrid_grad_norm (a model's tensors in
+ *            several lists) make one step.
+ * HG_ERR_INVALID_ARG as hashgrid_adam_step, and where an array that is written shares memory with another one of the call. */
+hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam_tensor* tensors, float grad_scale, int zero_grad,
+                              uint32_t step, hashgrid_grad_stats* stats, void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* hashgrid_strerror(hg_status s);
 

@@ -8,6 +8,7 @@ entry points raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 
@@ -16,7 +17,7 @@ import torch  # imported before the library so that both share one HIP runtime
 from .build import LIB_PATH, PROBES_LIB_PATH
 
 HG_OK = 0
-HG_F32, HG_F16 = 0, 1
+HG_F32, HG_F16, HG_BF16 = 0, 1, 2
 HG_INTERP_LINEAR, HG_INTERP_SMOOTHSTEP = 0, 1
 HG_MAX_LEVELS = 32
 HG_BWD_COUNTED = 1
@@ -25,10 +26,12 @@ HG_ERR_UNSUPPORTED = 2
 HG_STATIC_SCRATCH_BYTES = 64 << 20
 HG_LOSS_L2, HG_LOSS_MAPE = 0, 1
 HG_TRAIN_SCRATCH_BYTES = 256 * (8 + 40 * 1024)
+HG_GRAD_STATS_BYTES = 32 + 2048 * 8
 _LOSSES = {"l2": HG_LOSS_L2, "mape": HG_LOSS_MAPE, HG_LOSS_L2: HG_LOSS_L2, HG_LOSS_MAPE: HG_LOSS_MAPE}
 
 _DTYPES = {"f32": HG_F32, "f16": HG_F16, torch.float32: HG_F32, torch.float16: HG_F16}
 _TORCH = {HG_F32: torch.float32, HG_F16: torch.float16}
+_LIST_DTYPES = {torch.float32: HG_F32, torch.float16: HG_F16, torch.bfloat16: HG_BF16}  # of the lists of tensors
 
 EXPORTS = ("hashgrid_create", "hashgrid_destroy", "hashgrid_n_entries", "hashgrid_level_info",
            "hashgrid_encode_fwd", "hashgrid_encode_bwd", "hashgrid_encode_bwd_input",
@@ -36,7 +39,8 @@ EXPORTS = ("hashgrid_create", "hashgrid_destroy", "hashgrid_n_entries", "hashgri
            "hashgrid_encode_bwd_ws", "hashgrid_encode_fwd_ws", "hashgrid_bwd_ws_pays", "hashgrid_adam_step",
            "hashgrid_encode_mlp_fwd", "hashgrid_encode_bwd_static", "hashgrid_encode_mlp_fwd_train", "hashgrid_mlp_bwd",
            "hashgrid_adam_step_half_grad", "hashgrid_loss_grad", "hashgrid_mlp_fwd",
-           "hashgrid_encode_mlp_bwd_input", "hashgrid_train_step")
+           "hashgrid_encode_mlp_bwd_input", "hashgrid_train_step", "hashgrid_grad_norm", "hashgrid_clip_grads",
+           "hashgrid_adam_steps")
 PROBE_EXPORTS = ("hashgrid_probe_copy", "hashgrid_probe_gather", "hashgrid_probe_atomic_add",
                  "hashgrid_probe_gather_lines")
 
@@ -52,6 +56,16 @@ class hashgrid_config(ctypes.Structure):
 
 class hashgrid_adam_config(ctypes.Structure):
     _fields_ = [(n, ctypes.c_float) for n in ("lr", "beta1", "beta2", "eps", "l2_reg")]
+
+
+class hashgrid_grad(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_scalars", ctypes.c_uint64), ("dtype", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class hashgrid_adam_tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("params_master", "params_half", "grad", "m", "v")] + \
+               [("n_scalars", ctypes.c_uint64), ("grad_dtype", ctypes.c_uint32), ("half_dtype", ctypes.c_uint32),
+                ("cfg", hashgrid_adam_config), ("reserved", ctypes.c_uint32)]
 
 
 class hashgrid_train_state(ctypes.Structure):
@@ -124,6 +138,12 @@ def load_library() -> ctypes.CDLL:
     lib.hashgrid_encode_mlp_bwd_input.restype = ctypes.c_int
     lib.hashgrid_train_step.argtypes = [vp, ctypes.POINTER(hashgrid_train_state), u32, vp, vp, vp, vp, vp, u64, u32, vp]
     lib.hashgrid_train_step.restype = ctypes.c_int
+    lib.hashgrid_grad_norm.argtypes = [u32, vp, ctypes.c_float, ctypes.c_float, vp, vp]
+    lib.hashgrid_grad_norm.restype = ctypes.c_int
+    lib.hashgrid_clip_grads.argtypes = [u32, vp, vp, vp, vp]
+    lib.hashgrid_clip_grads.restype = ctypes.c_int
+    lib.hashgrid_adam_steps.argtypes = [u32, vp, ctypes.c_float, ctypes.c_int, u32, vp, vp]
+    lib.hashgrid_adam_steps.restype = ctypes.c_int
     lib.hashgrid_strerror.argtypes = [ctypes.c_int]
     lib.hashgrid_strerror.restype = ctypes.c_char_p
     _lib = lib
@@ -442,6 +462,172 @@ def adam_step(params_master: torch.Tensor, grad: torch.Tensor, m: torch.Tensor, 
         _check(lib.hashgrid_adam_step(n, params_master.data_ptr(), half_ptr, grad.data_ptr(), m.data_ptr(),
                                       v.data_ptr(), ctypes.byref(cfg), step, int(zero_grad), _stream_ptr(stream)),
                "hashgrid_adam_step")
+
+
+class GradStats:
+    """What grad_norm leaves on the device for the calls after it (hashgrid_grad_stats); one per model.
+      norm    fp32 [1]   the gradients' norm
+      factor  fp32 [1]   min(1, max_norm / norm); 0 where a gradient is not finite
+      step    int32 [1]  number of the optimiser step that is due; 0 where it is left out because a gradient is not finite
+      steps   int32 [1]  optimiser steps taken by adam_steps; set it (steps.fill_(n)) to resume
+    Views of device memory: reading one as a number waits for the stream."""
+
+    def __init__(self, device=None):
+        self.memory = torch.zeros(HG_GRAD_STATS_BYTES, dtype=torch.uint8, device="cuda" if device is None else device)
+        word = [self.memory[4 * i:4 * i + 4] for i in range(4)]
+        self.norm, self.factor = word[0].view(torch.float32), word[1].view(torch.float32)
+        self.step, self.steps = word[2].view(torch.int32), word[3].view(torch.int32)
+
+
+def _on_current_device(device, what: str) -> None:
+    if device is not None and device != _current_device():
+        raise HashGridError(f"{what} on device {device}, the current device is {_current_device()}")
+
+
+def _stats_ptr(stats) -> int:
+    if not isinstance(stats, GradStats):
+        raise HashGridError("stats must be a GradStats")
+    _on_current_device(stats.memory.get_device(), "stats")
+    return stats.memory.data_ptr()
+
+
+class GradList:
+    """Gradients of a model, of any shapes, fp32, fp16 and bf16 mixed, looked over once for many calls.  The tensors keep their
+    sizes and types; one whose memory has moved since the last call is looked up again."""
+
+    def __init__(self, grads):
+        self.tensors = list(grads)
+        self._look_up()
+
+    def _look_up(self):
+        devices = set()
+        for i, t in enumerate(self.tensors):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype in _LIST_DTYPES):
+                raise HashGridError(f"tensor {i} of the list must be a contiguous fp32, fp16 or bf16 device tensor")
+            devices.add(t.get_device())
+        if len(devices) > 1:
+            raise HashGridError("the tensors of a list must be on one device")
+        self._device = devices.pop() if devices else None
+        self._at = [t.data_ptr() for t in self.tensors]
+        self._kinds = [(t.dtype, t.numel()) for t in self.tensors]
+        self._pointers = (ctypes.c_void_p * len(self._at))(*self._at)
+        self._array = (hashgrid_grad * len(self._at))(*[(at, n, _LIST_DTYPES[dtype], 0)
+                                                        for at, (dtype, n) in zip(self._at, self._kinds)])
+
+    def _current(self):
+        if [t.data_ptr() for t in self.tensors] != self._at:
+            self._look_up()
+        _on_current_device(self._device, "tensors")
+        return self
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _grad_list(grads) -> GradList:
+    return (grads if isinstance(grads, GradList) else GradList(grads))._current()
+
+
+def grad_norm(grads, stats: GradStats, max_norm: float = math.inf, grad_scale: float = 1.0, stream=None) -> torch.Tensor:
+    """hashgrid_grad_norm over a GradList or any sequence of tensors: returns stats.norm, grad_scale times the Euclidean
+    norm of all scalars; stats.factor is what brings it down to max_norm."""
+    g = _grad_list(grads)
+    _check(load_library().hashgrid_grad_norm(len(g), g._array, grad_scale, max_norm, _stats_ptr(stats), _stream_ptr(stream)),
+           "hashgrid_grad_norm")
+    return stats.norm
+
+
+def clip_grads(grads, max_norm: float, stats: GradStats, out=None, grad_scale: float = 1.0, stream=None) -> torch.Tensor:
+    """grad_norm, then hashgrid_clip_grads: the gradients times stats.factor, in place or into the tensors of `out` (of the same
+    types and sizes); gradients that are not all finite become zeros.  They keep their loss scale.  Returns stats.norm, as
+    it was before.  (adam_steps clips on its way and needs grad_norm alone.)"""
+    g = _grad_list(grads)
+    to = None if out is None else _grad_list(out)
+    if to is not None and to._kinds != g._kinds:
+        raise HashGridError("out must be tensors of the gradients' types and sizes")
+    norm = grad_norm(g, stats, max_norm, grad_scale, stream)
+    _check(load_library().hashgrid_clip_grads(len(g), g._array, None if to is None else to._pointers, _stats_ptr(stats),
+                                              _stream_ptr(stream)), "hashgrid_clip_grads")
+    return norm
+
+
+@dataclass
+class AdamTensor:
+    """One tensor of adam_steps: fp32 master copy and moments, gradient (fp32, fp16 or bf16), 16-bit working copy or None, and
+    the hyper-parameters, which may be changed between steps."""
+    params_master: torch.Tensor
+    grad: torch.Tensor
+    m: torch.Tensor
+    v: torch.Tensor
+    params_half: torch.Tensor | None = None
+    lr: float = 1e-2
+    beta1: float = 0.9
+    beta2: float = 0.99
+    eps: float = 1e-15
+    l2_reg: float = 0.0
+
+    def _key(self):
+        h = self.params_half
+        return (self.params_master.data_ptr(), None if h is None else h.data_ptr(), self.grad.data_ptr(), self.m.data_ptr(),
+                self.v.data_ptr(), self.lr, self.beta1, self.beta2, self.eps, self.l2_reg)
+
+
+class AdamList:
+    """The tensors of a model that one optimiser step updates, looked over once for many calls; a tensor that was replaced, whose
+    memory has moved or whose hyper-parameters have changed is looked up again.  grads: their GradList."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self._grads = None
+        self._look_up()
+
+    def _look_up(self):
+        devices, rows = set(), []
+        for i, t in enumerate(self.tensors):
+            n = t.grad.numel()
+            for name, a, types in (("params_master", t.params_master, (torch.float32,)), ("m", t.m, (torch.float32,)),
+                                   ("v", t.v, (torch.float32,)), ("grad", t.grad, tuple(_LIST_DTYPES)),
+                                   ("params_half", t.params_half, (torch.float16, torch.bfloat16))):
+                if name == "params_half" and a is None:
+                    continue
+                if not (a.is_cuda and a.is_contiguous() and a.dtype in types and a.numel() == n):
+                    raise HashGridError(f"{name} of tensor {i} must be a contiguous device tensor of {n} scalars, {types}")
+                devices.add(a.get_device())
+            half = HG_F16 if t.params_half is None else _LIST_DTYPES[t.params_half.dtype]
+            key = t._key()
+            rows.append((*key[:5], n, _LIST_DTYPES[t.grad.dtype], half, hashgrid_adam_config(*key[5:]), 0))
+        if len(devices) > 1:
+            raise HashGridError("the tensors of a list must be on one device")
+        self._device = devices.pop() if devices else None
+        self._keys = [t._key() for t in self.tensors]
+        self._array = (hashgrid_adam_tensor * len(rows))(*rows)
+
+    def _current(self):
+        if [t._key() for t in self.tensors] != self._keys:
+            self._look_up()
+        _on_current_device(self._device, "tensors")
+        return self
+
+    @property
+    def grads(self) -> GradList:
+        known = self._grads
+        if known is None or any(t.grad is not g for t, g in zip(self.tensors, known.tensors)):
+            known = self._grads = GradList([t.grad for t in self.tensors])
+        return known
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def adam_steps(tensors, stats: GradStats | None = None, step: int = 0, zero_grad: bool = True, grad_scale: float = 1.0,
+               stream=None) -> None:
+    """hashgrid_adam_steps on an AdamList or any sequence of AdamTensor: adam_step on all of them in one launch.  With
+    stats, after grad_norm over the same gradients: they are clipped on the way, the step is left out where one of them is not
+    finite, and the device counts the steps.  Without: the step's number is `step`, counted from 1."""
+    a = (tensors if isinstance(tensors, AdamList) else AdamList(tensors))._current()
+    _check(load_library().hashgrid_adam_steps(len(a), a._array, grad_scale, int(zero_grad), step,
+                                              None if stats is None else _stats_ptr(stats), _stream_ptr(stream)),
+           "hashgrid_adam_steps")
 
 
 def loss_grad(prediction: torch.Tensor, target: torch.Tensor, loss, scale: float, dLdout: torch.Tensor,

@@ -1,0 +1,404 @@
+"""hashgrid_grad_norm, hashgrid_clip_grads and hashgrid_adam_steps through the binding against oracle/grad_norm_oracle.py (extended
+precision) and the fp64 optimiser oracle, on lists of tensors of several types, sizes and alignments.
+
+Bars.  norm: squares and sums in 64 bits (a chain of at most 10^5 additions: 10^5 2^-53 < 2^-36 relative), rounded once to fp32:
+2^-24 relative, here 2^-24 (1 + 2^-10), and half the smallest subnormal.  factor: one 64-bit quotient rounded once: the same.  Clipped
+gradients: one fp32 product with the factor on the device, rounded once to the type: bit for bit what torch gives.  The
+optimiser step: bit for bit hashgrid_adam_step's where both get the same gradient and the same step number from the host; against
+the oracle the bars of test_gpu_adam.py, with the gradient's own two roundings (scale, product: 2^-23 relative) on top.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import grad_norm_oracle as gno
+from oracle import hashgrid_oracle as orc
+from paper_2201_05989_amd import AdamList, AdamTensor, GradList, GradStats, HashGridError, adam_step, adam_steps, clip_grads, grad_norm
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+HALF_ULP = 2.0 ** -24 * (1 + 2.0 ** -10)
+
+
+def cpu64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def make(sizes, dtype, seed, shift=0, scale=1.0, guard=None):
+    """Tensors laid one after the other, `shift` scalars into an allocation: any alignment an element may have."""
+    rng = np.random.default_rng(seed)
+    n = sum(sizes)
+    flat = torch.empty(n + shift + 8, dtype=dtype, device="cuda")
+    if guard is not None:
+        flat.fill_(guard)
+    values = rng.standard_normal(n) * 10.0 ** rng.uniform(-4, 0, n) * scale
+    values[rng.random(n) < 0.2] = 0.0
+    flat[shift:shift + n] = torch.from_numpy(values).cuda().to(dtype)
+    out, at = [], shift
+    for k in sizes:
+        out.append(flat[at:at + k])
+        at += k
+    return flat, out
+
+
+def check_norm(grads, stats, max_norm, grad_scale=1.0):
+    want = gno.norm([cpu64(g) for g in grads], grad_scale)
+    norm, factor, step = float(stats.norm), float(stats.factor), int(stats.step)
+    assert abs(norm - want) <= HALF_ULP * want + 2.0 ** -150, (norm, want)
+    want_factor = gno.factor(want, float(np.float32(max_norm)))  # the bound is an fp32 argument: the caller's number, rounded
+    assert abs(factor - want_factor) <= HALF_ULP * want_factor + 2.0 ** -150, (factor, want_factor)
+    assert step == int(stats.steps) + 1
+
+
+LISTS = [[1], [0], [], [2047], [2048], [2049], [0, 5, 0, 1], [7, 4096, 1, 1, 300, 65537], [100003, 3], [1] * 300, list(range(1, 140)),
+         [5_300_017, 11, 2049, 900_001]]
+
+
+@pytest.mark.parametrize("sizes", LISTS, ids=lambda s: f"{len(s)}x{sum(s)}")
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_norm_of_any_list(kind, sizes):
+    for shift in (0, 1, 3):
+        _, grads = make(sizes, TYPES[kind], len(sizes) + shift, shift)
+        stats = GradStats()
+        returned = grad_norm(grads, stats, max_norm=0.25)
+        assert returned is stats.norm
+        check_norm(grads, stats, 0.25)
+        bits = stats.memory[:16].clone()
+        grad_norm(GradList(grads), stats, max_norm=0.25)
+        assert torch.equal(bits, stats.memory[:16])  # the same arrays give the same bits
+
+
+def test_norm_of_mixed_types_and_shapes_with_a_loss_scale():
+    a = torch.randn(37, 5, 11, device="cuda")
+    b = (torch.randn(1001, 64, device="cuda") * 128).half()
+    c = torch.randn(3, device="cuda").bfloat16()
+    d = torch.randn((), device="cuda")
+    stats = GradStats()
+    for scale in (1.0, 1.0 / 128.0, 3.0):
+        for bound in (0.0, 1e-3, 1e9, float("inf")):
+            grad_norm([a, b, c, d, a], stats, bound, scale)   # the same tensor twice counts twice
+            check_norm([a, b, c, d, a], stats, bound, scale)
+
+
+@pytest.mark.parametrize("value,kind", [(1e30, "f32"), (3e38, "f32"), (1e-30, "f32"), (1e-44, "f32"), (65504.0, "f16"), (6e-8, "f16"),
+                                        (3e38, "bf16"), (1e-40, "bf16"), (0.0, "f32")])
+def test_no_gradient_is_too_large_or_too_small(value, kind):
+    g = torch.full((100_003,), value, dtype=TYPES[kind], device="cuda")
+    g[0] = 0.0
+    stats = GradStats()
+    bound = 1.0
+    grad_norm([g], stats, bound)
+    want = gno.norm([cpu64(g)])
+    norm = float(stats.norm)
+    if want > torch.finfo(torch.float32).max * (1 + 2.0 ** -24):
+        assert norm == float("inf") and int(stats.step) == 1   # the gradients are finite: only the norm's type is too small
+    else:
+        assert abs(norm - want) <= HALF_ULP * want + 2.0 ** -150
+    f = gno.factor(want, bound)
+    assert abs(float(stats.factor) - f) <= HALF_ULP * f + 2.0 ** -150
+    out = torch.empty_like(g)
+    clip_grads([g], bound, stats, out=[out])
+    # subnormals as anywhere: rounded, not flushed
+    assert torch.equal(out, torch.zeros_like(g) if float(stats.factor) == 0 else (g.float() * stats.factor).to(g.dtype))
+
+
+CLIPS = [[1], [0, 3], [2049, 1, 7], [7, 4096, 1, 1, 300, 65537], [9] * 200, [3_000_001, 65]]
+
+
+@pytest.mark.parametrize("sizes", CLIPS, ids=lambda s: f"{len(s)}x{sum(s)}")
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_clipping_in_place_and_into_other_arrays(kind, sizes):
+    for shift, out_shift in ((0, 0), (1, 1), (2, 3)):
+        flat, grads = make(sizes, TYPES[kind], 7, shift, guard=9.0)
+        before = flat.clone()
+        big, outs = make(sizes, TYPES[kind], 8, out_shift, guard=7.0)
+        rest = torch.ones_like(big, dtype=torch.bool)
+        rest[out_shift:out_shift + sum(sizes)] = False
+        stats = GradStats()
+        for bound in (0.01, 1e9, 0.0):
+            clip_grads(grads, bound, stats, out=outs)
+            check_norm(grads, stats, bound)
+            for g, o in zip(grads, outs):
+                assert torch.equal(o, (g.float() * stats.factor).to(g.dtype))
+            assert torch.equal(flat, before) and bool((big[rest] == 7.0).all())
+        clip_grads(grads, 1e9, stats)          # nothing to clip
+        assert torch.equal(flat, before)
+        norm = clip_grads(grads, 0.01, stats)  # in place
+        assert norm is stats.norm
+        want = before.clone()
+        want[shift:shift + sum(sizes)] = (before[shift:shift + sum(sizes)].float() * stats.factor).to(before.dtype)
+        assert torch.equal(flat, want)         # what lies around the tensors too
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_gradients_that_are_not_finite_leave_the_step_out(kind, bad):
+    sizes = [5, 70_001, 2048]
+    for where in (0, 4, 5, 40_000, 72_053):
+        flat, grads = make(sizes, TYPES[kind], 3)
+        items = []
+        for g in grads:
+            n = g.numel()
+            items.append(AdamTensor(torch.randn(n, device="cuda"), g, torch.rand(n, device="cuda"), torch.rand(n, device="cuda"), l2_reg=0.1))
+            items[-1].params_half = items[-1].params_master.half()
+        model = AdamList(items)
+        stats = GradStats()
+        stats.steps.fill_(11)
+        flat[where] = bad
+        grad_norm(model.grads, stats, 1.0)
+        assert not np.isfinite(float(stats.norm)) and float(stats.factor) == 0.0 and int(stats.step) == 0
+        outs = [torch.full_like(g, 3.0) for g in grads]
+        clip_grads(grads, 1.0, stats, out=outs)
+        assert all(bool((o == 0).all()) for o in outs)
+        before = [[a.clone() for a in (t.params_master, t.params_half, t.m, t.v)] for t in items]
+        kept = flat.clone()
+        adam_steps(model, stats, zero_grad=False)
+        assert torch.equal(flat.view(torch.uint8), kept.view(torch.uint8))
+        adam_steps(model, stats)
+        for t, was in zip(items, before):
+            assert all(torch.equal(a, b) for a, b in zip((t.params_master, t.params_half, t.m, t.v), was))
+        assert bool((flat[:sum(sizes)] == 0).all()) and int(stats.steps) == 11
+        # the next gradients are finite: step 12
+        for g in grads:
+            g.copy_(torch.ones(g.numel(), device="cuda"))
+        grad_norm(model.grads, stats, 1.0)
+        assert int(stats.step) == 12
+        adam_steps(model, stats)
+        assert int(stats.steps) == 12 and not torch.equal(items[1].params_master, before[1][0])
+
+
+def test_clip_in_place_of_gradients_that_are_not_finite_gives_zeros():
+    g = torch.ones(5000, device="cuda")
+    g[77] = float("inf")
+    stats = GradStats()
+    clip_grads([g], float("inf"), stats)
+    assert bool((g == 0).all())
+
+
+def tensors_for_adam(sizes, kinds, seed, shift, l2):
+    rng = np.random.default_rng(seed)
+    items = []
+    for i, n in enumerate(sizes):
+        kind = kinds[i % len(kinds)]
+        scale = 100.0 if kind == "f16" else 1.0
+        _, (g,) = make([n], TYPES[kind], seed + i, shift, scale)
+        arrays = [torch.from_numpy(a.astype(np.float32)).cuda() for a in
+                  (rng.standard_normal(n + shift) * 0.1, rng.standard_normal(n + shift) * 1e-3, rng.random(n + shift) * 1e-4)]
+        p, m, v = (a[shift:] for a in arrays)
+        half = None if i % 4 == 3 else p.to(torch.bfloat16 if i % 4 == 2 else torch.float16)
+        items.append(AdamTensor(p, g, m, v, half, lr=1e-2 if i % 2 else 1e-3, beta1=0.9 if i % 3 else 0.8, l2_reg=l2 if i % 2 else 0.0))
+    return items
+
+
+ADAMS = [([1], ["f32"], 0), ([3, 4, 5], ["f32", "f16", "bf16"], 0), ([0, 2047, 2049, 1], ["bf16", "f32", "f16"], 1),
+         ([100_003, 17, 5000], ["f32", "f16"], 0), ([100_003, 17, 5000], ["f16", "f32"], 3), (list(range(1, 120)), ["f32", "f16", "bf16"], 1),
+         ([2_500_001, 6208], ["f32"], 0)]
+
+
+@pytest.mark.parametrize("sizes,kinds,shift", ADAMS, ids=lambda a: str(len(a)) if isinstance(a, list) else str(a))
+@pytest.mark.parametrize("bound", [0.05, 1e9])
+def test_clipped_steps_against_the_oracle(sizes, kinds, shift, bound):
+    items = tensors_for_adam(sizes, kinds, 5, shift, 1e-3)
+    model, stats = AdamList(items), GradStats()
+    stats.steps.fill_(2)
+    grad_scale = 0.25
+    for step, zero in ((3, False), (4, True)):
+        state = [[cpu64(a) for a in (t.params_master, t.m, t.v, t.grad)] for t in items]
+        halves = [None if t.params_half is None else t.params_half.clone() for t in items]
+        grad_norm(model.grads, stats, bound, grad_scale)
+        check_norm([t.grad for t in items], stats, bound, grad_scale)
+        factor = float(gno.factor(gno.norm([s[3] for s in state], grad_scale), float(np.float32(bound))))
+        adam_steps(model, stats, grad_scale=grad_scale, zero_grad=zero)
+        assert int(stats.steps) == step
+        for t, (p, m, v, raw), half in zip(items, state, halves):
+            g = raw * (grad_scale * factor)
+            l2, beta1, beta2 = (float(np.float32(a)) for a in (t.l2_reg, t.beta1, t.beta2))
+            mass = np.abs(g) + l2 * np.abs(p)
+            # fp32: m and v sum two terms of two or three roundings, the gradient itself carries three (its scale, product and sum)
+            m_bar = 2e-6 * (beta1 * np.abs(m) + (1 - beta1) * mass) + 1e-37
+            v_bar = 2e-6 * (beta2 * v + (1 - beta2) * mass ** 2) + 1e-37
+            p0 = p.copy()
+            orc.adam_step(p, g, m, v, lr=float(np.float32(t.lr)), beta1=beta1, beta2=beta2, step=step, l2=l2)
+            got = [cpu64(a) for a in (t.params_master, t.m, t.v)]
+            assert (np.abs(got[1] - m) <= m_bar).all() and (np.abs(got[2] - v) <= v_bar).all()
+            # the update lr m^ / sqrt(v^): the relative errors of both, 4 roundings, and the rounding of p
+            c1, c2 = 1 - beta1 ** step, 1 - beta2 ** step
+            with np.errstate(divide="ignore", invalid="ignore"):
+                root = np.sqrt(v / c2) + 1e-15
+                p_bar = t.lr / c1 * (m_bar + np.abs(m) * (v_bar / v + 4e-7)) / root + 6e-8 * (np.abs(p) + np.abs(p0))
+            live = raw * grad_scale + l2 * p0 != 0
+            assert (np.abs(got[0] - p)[live] <= p_bar[live]).all()
+            assert np.array_equal(got[0][~live], p0[~live])
+            if half is not None:
+                assert torch.equal(t.params_half, t.params_master.to(half.dtype))
+            assert bool((t.grad == 0).all()) if zero else np.array_equal(cpu64(t.grad), raw)
+
+
+@pytest.mark.parametrize("n,kind,l2,zero", [(1, "f32", 0.0, True), (1027, "f32", 1e-2, True), (100_003, "f32", 0.0, False), (100_003, "f16", 0.0, True),
+                                            (6208, "f16", 1e-6, True)])
+def test_one_tensor_and_a_step_of_the_hosts_is_adam_step_bit_for_bit(n, kind, l2, zero):
+    for step in (1, 2, 1000):
+        _, (g,) = make([n], TYPES[kind], step)
+        p, m, v = torch.randn(n, device="cuda"), torch.randn(n, device="cuda") * 1e-3, torch.rand(n, device="cuda") * 1e-4
+        a = [t.clone() for t in (p, g, m, v)] + [p.half()]
+        b = [t.clone() for t in (p, g, m, v)] + [p.half()]
+        scale = 0.5 if kind == "f16" else 1.0
+        adam_step(*a[:4], step, params_half=a[4], zero_grad=zero, grad_scale=scale, l2_reg=l2)
+        adam_steps([AdamTensor(*b, l2_reg=l2)], step=step, zero_grad=zero, grad_scale=scale)
+        assert all(torch.equal(s, t) for s, t in zip(a, b))
+
+
+def test_several_lists_after_one_norm_make_one_step():
+    items = tensors_for_adam([500, 300, 7], ["f32"], 9, 0, 0.0)
+    stats = GradStats()
+    adam_steps(items, stats)  # no norm has been taken: nothing is updated
+    assert int(stats.steps) == 0
+    grad_norm([t.grad for t in items], stats)
+    before = [t.params_master.clone() for t in items]
+    adam_steps(items, stats)  # (the gradients are zero now: that first call has cleared them)
+    assert int(stats.steps) == 1 and all(torch.equal(t.params_master, b) for t, b in zip(items, before))
+    for t in items:
+        t.grad.fill_(1.0)
+    grad_norm([t.grad for t in items], stats)
+    adam_steps(items[:1], stats)
+    adam_steps(items[1:], stats)
+    assert int(stats.steps) == 2 and all(not torch.equal(t.params_master, b) for t, b in zip(items, before))
+    adam_steps([], stats)
+    assert int(stats.steps) == 2
+
+
+def test_lists_follow_tensors_that_move_and_hyper_parameters_that_change():
+    items = tensors_for_adam([5000, 64], ["f32"], 4, 0, 0.0)
+    model, stats = AdamList(items), GradStats()
+    grad_norm(model.grads, stats)
+    first = float(stats.norm)
+    items[0].grad = items[0].grad * 2       # another tensor
+    items[1].grad.data = items[1].grad * 2  # other memory
+    grad_norm(model.grads, stats)
+    assert abs(float(stats.norm) - 2 * first) <= 2e-7 * first
+    items[0].lr = 0.0
+    before = [t.params_master.clone() for t in items]
+    adam_steps(model, stats)
+    assert torch.equal(items[0].params_master, before[0]) and not torch.equal(items[1].params_master, before[1])
+    g = GradList([torch.ones(4, device="cuda")])
+    g.tensors[0].data = torch.ones(4)       # host memory: refused, and no sooner
+    with pytest.raises(HashGridError):
+        grad_norm(g, stats)
+
+
+def test_another_stream_and_a_captured_step():
+    """norm, clipping and the optimiser step recorded once and replayed on other gradients, with eager work between the replays,
+    against the same calls made one by one; the device counts the steps."""
+    sizes, kinds = [70_001, 5, 2048, 333], ["f32", "f16", "bf16"]
+    a, b = (tensors_for_adam(sizes, kinds, 21, 1, 1e-3) for _ in range(2))
+    A, B = AdamList(a), AdamList(b)
+    sa, sb = GradStats(), GradStats()
+    outs = [[torch.empty_like(t.grad) for t in x] for x in (a, b)]
+    stream = torch.cuda.Stream()
+
+    def step(model, stats, out):
+        clip_grads(model.grads, 0.05, stats, out=out)
+        adam_steps(model, stats, zero_grad=True)
+
+    graph = torch.cuda.CUDAGraph()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        step(A, sa, outs[0])
+    torch.cuda.synchronize()
+    for i in range(5):
+        gen = torch.Generator(device="cuda").manual_seed(i)
+        for s, t in zip(a, b):
+            new = torch.randn(s.grad.numel(), device="cuda", generator=gen)
+            if i == 2:
+                new[0] = float("nan")
+            s.grad.copy_(new)
+            t.grad.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        other = torch.cuda.Stream()
+        with torch.cuda.stream(other):
+            other.wait_stream(torch.cuda.default_stream())
+            step(B, sb, outs[1])
+        other.synchronize()
+        torch.randn(1000, device="cuda").sum().item()
+        assert torch.equal(sa.memory[4:16], sb.memory[4:16]) and int(sa.steps) == (i + 1 if i < 2 else i)
+        for s, t in zip(a, b):
+            for x, y in zip((s.params_master, s.m, s.v, s.grad), (t.params_master, t.m, t.v, t.grad)):
+                assert torch.equal(x, y)
+        assert all(torch.equal(x, y) for x, y in zip(*outs))
+
+
+def test_a_stream_given_as_an_argument():
+    g = torch.randn(100_003, device="cuda")
+    want = g.clone()
+    stats, stream = GradStats(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    item = AdamTensor(torch.zeros_like(g), g, torch.zeros_like(g), torch.zeros_like(g))
+    clip_grads([g], 1.0, stats, stream=stream)
+    adam_steps([item], stats, zero_grad=False, stream=stream)
+    stream.synchronize()
+    assert torch.equal(g, want * stats.factor) and int(stats.steps) == 1 and bool((item.m != 0).any())
+
+
+def test_arrays_beyond_32_bits():
+    n = (1 << 32) + 4099
+    g = torch.zeros(n, dtype=torch.float16, device="cuda")
+    where = torch.tensor([0, 1 << 31, (1 << 32) - 1, 1 << 32, n - 1], device="cuda")
+    g[where] = torch.tensor([3.0, 4.0, 12.0, 84.0, 132.0], dtype=torch.float16, device="cuda")
+    stats = GradStats()
+    clip_grads([g], 15.7, stats)   # 3, 4, 12, 84, 132: norm 157
+    assert float(stats.norm) == 157.0 and abs(float(stats.factor) - 0.1) <= 1e-8
+    assert torch.equal(g[where], (torch.tensor([3.0, 4.0, 12.0, 84.0, 132.0], device="cuda") * stats.factor).half())
+    assert int(torch.count_nonzero(g)) == 5
+    del g
+    n = (1 << 30) + 1031
+    g = torch.zeros(n, device="cuda", dtype=torch.float16)
+    where = torch.tensor([0, (1 << 30) - 1, 1 << 30, n - 1], device="cuda")
+    g[where] = 1.0
+    p, m, v = (torch.zeros(n, device="cuda") for _ in range(3))
+    grad_norm([g], stats)
+    adam_steps([AdamTensor(p, g, m, v)], stats)
+    for t, want in ((p, -1e-2), (m, 0.1), (v, 0.01)):
+        assert int(torch.count_nonzero(t)) == 4 and bool(((t[where] - want).abs() <= 1e-6 * abs(want)).all())
+    assert not bool(g.any())
+
+
+def test_refusals():
+    g = torch.zeros(64, device="cuda")
+    stats = GradStats()
+    for bad in ([g[::2]], [g.double()], [g.cpu()], [g.int()], [None], [3.0]):
+        with pytest.raises(HashGridError):
+            grad_norm(bad, stats)
+    for kw in ({"grad_scale": 0.0}, {"grad_scale": float("inf")}, {"grad_scale": -1.0}, {"max_norm": -1.0}, {"max_norm": float("nan")}):
+        with pytest.raises(HashGridError):
+            grad_norm([g], stats, **kw)
+    with pytest.raises(HashGridError):
+        grad_norm([g], stats.memory)
+    with pytest.raises(HashGridError):
+        grad_norm([g] * 1025, stats)
+    for out in ([g, g], [g[:32]], [g.half()], [g[::2]]):
+        with pytest.raises(HashGridError):
+            clip_grads([g], 1.0, stats, out=out)
+    h = torch.zeros(100, device="cuda")
+    for grads, out in (([g, g], None), ([h[:60], h[50:]], None), ([h[:60]], [h[1:61]]), ([h[:20], h[20:40]], [h[20:40], h[:20]]),
+                       ([h[:20], h[20:40]], [g[:20], g[:20]])):
+        with pytest.raises(HashGridError):
+            clip_grads(grads, 1.0, stats, out=out)
+    clip_grads([g, g], 1.0, stats, out=[h[:64], torch.empty_like(g)])  # the same tensor twice, read only
+    clip_grads([h[:20], h[20:40]], 1.0, stats, out=[h[:20], g[:20]])   # in place for one of them
+    p, m, v = (torch.zeros(64, device="cuda") for _ in range(3))
+    good = dict(params_master=p, grad=g, m=m, v=v)
+    for change in ({"grad": g[:32]}, {"m": m.half()}, {"v": v.cpu()}, {"params_half": p}, {"beta1": 1.0}, {"eps": -1.0}, {"l2_reg": float("inf")},
+                   {"v": m}, {"params_master": g}):
+        with pytest.raises(HashGridError):
+            adam_steps([AdamTensor(**{**good, **change})], step=1)
+    for kw in ({"step": 0}, {"step": 1, "stats": stats}, {"step": 1, "grad_scale": 0.0}):
+        with pytest.raises(HashGridError):
+            adam_steps([AdamTensor(**good)], **kw)
+    with pytest.raises(HashGridError):
+        adam_steps([AdamTensor(**good), AdamTensor(**good)], step=1)
+    shared = AdamTensor(torch.zeros_like(p), g, torch.zeros_like(p), torch.zeros_like(p))
+    adam_steps([AdamTensor(**good), shared], step=1, zero_grad=False)  # a gradient that two tensors share is only read
+    with pytest.raises(HashGridError):
+        adam_steps([AdamTensor(**good), shared], step=1)
