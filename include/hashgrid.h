@@ -400,8 +400,9 @@ hg_status hashgrid_train_step(const hashgrid_t* hg, const hashgrid_train_state* 
  * training loop does not wait and a whole step can be captured into a graph and replayed, the optimiser's step number included. */
 #define HG_BF16 2u                           /* beside HG_F32 and HG_F16, in the lists below only */
 #define HG_MAX_TENSORS 1024u                 /* tensors a call; more returns HG_ERR_UNSUPPORTED */
-#define HG_MAX_TENSOR_SCALARS (1ull << 42)   /* scalars a tensor; as all tensors of a call together */
+#define HG_MAX_TENSOR_SCALARS (1ull << 42)   /* scalars a tensor, and all tensors of a call together */
 #define HG_GRAD_NORM_GROUPS 2048u
+#define HG_GRAD_NORM_GATES 33u
 
 typedef struct {
   void* data;         /* device, aligned to its element; not looked at when n_scalars == 0 */
@@ -416,8 +417,9 @@ typedef struct {
   float factor;    /* min(1, max_norm / norm); 0 where the sum of the squares is not finite */
   uint32_t step;   /* number of the optimiser step that is due: steps + 1, or 0 where the sum is not finite: left out */
   uint32_t steps;  /* optimiser steps taken (hashgrid_adam_steps).  A caller that resumes sets it. */
-  uint32_t scratch[4];
-  double partials[HG_GRAD_NORM_GROUPS]; /* scratch */
+  uint32_t reserved[28];
+  uint32_t arrived[HG_GRAD_NORM_GATES][32]; /* scratch, all zero between calls */
+  double partials[HG_GRAD_NORM_GROUPS];     /* scratch */
 } hashgrid_grad_stats;
 
 /* norm = grad_scale * sqrt(sum of the squares of all scalars of all tensors) and what follows from it, into *stats.
@@ -431,14 +433,14 @@ typedef struct {
 hg_status hashgrid_grad_norm(uint32_t n_tensors, const hashgrid_grad* grads, float grad_scale, float max_norm,
                              hashgrid_grad_stats* stats, void* stream);
 
-/* out_i = factor * grads_i, each product rounded once to the tensor's type, with the factor that hashgrid_grad_norm has left in
- * *stats: the gradients keep their loss scale.  factor == 0 (max_norm 0, or a gradient that is not finite) writes zeros, which
- * hashgrid_adam_step passes over.
+/* hashgrid_grad_norm, and then out_i = factor * grads_i, each product rounded once to the tensor's type: the gradients keep their
+ * loss scale.  factor == 0 (max_norm 0, or a gradient that is not finite) writes zeros, which hashgrid_adam_step passes over.
+ * (hashgrid_adam_steps clips on its way and needs the norm alone.)
  *   out  [n_tensors]  HOST array of device pointers to arrays of the gradients' types and sizes; out[i] == grads[i].data
- *                     is in place.  NULL: all in place; where factor is 1 nothing is read or written then.
+ *                     is in place.  NULL: all in place; where factor is 1 nothing is written then.
  * HG_ERR_INVALID_ARG also where an array that is written shares memory with another one of the call. */
-hg_status hashgrid_clip_grads(uint32_t n_tensors, const hashgrid_grad* grads, void* const* out,
-                              const hashgrid_grad_stats* stats, void* stream);
+hg_status hashgrid_clip_grads(uint32_t n_tensors, const hashgrid_grad* grads, void* const* out, float grad_scale, float max_norm,
+                              hashgrid_grad_stats* stats, void* stream);
 
 typedef struct {
   float* params_master; /* [n] fp32, read and written (this and the other arrays: device, aligned to their element) */

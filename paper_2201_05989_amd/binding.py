@@ -26,7 +26,7 @@ HG_ERR_UNSUPPORTED = 2
 HG_STATIC_SCRATCH_BYTES = 64 << 20
 HG_LOSS_L2, HG_LOSS_MAPE = 0, 1
 HG_TRAIN_SCRATCH_BYTES = 256 * (8 + 40 * 1024)
-HG_GRAD_STATS_BYTES = 32 + 2048 * 8
+HG_GRAD_STATS_BYTES = 128 + 33 * 128 + 2048 * 8
 _LOSSES = {"l2": HG_LOSS_L2, "mape": HG_LOSS_MAPE, HG_LOSS_L2: HG_LOSS_L2, HG_LOSS_MAPE: HG_LOSS_MAPE}
 
 _DTYPES = {"f32": HG_F32, "f16": HG_F16, torch.float32: HG_F32, torch.float16: HG_F16}
@@ -140,7 +140,7 @@ def load_library() -> ctypes.CDLL:
     lib.hashgrid_train_step.restype = ctypes.c_int
     lib.hashgrid_grad_norm.argtypes = [u32, vp, ctypes.c_float, ctypes.c_float, vp, vp]
     lib.hashgrid_grad_norm.restype = ctypes.c_int
-    lib.hashgrid_clip_grads.argtypes = [u32, vp, vp, vp, vp]
+    lib.hashgrid_clip_grads.argtypes = [u32, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp]
     lib.hashgrid_clip_grads.restype = ctypes.c_int
     lib.hashgrid_adam_steps.argtypes = [u32, vp, ctypes.c_float, ctypes.c_int, u32, vp, vp]
     lib.hashgrid_adam_steps.restype = ctypes.c_int
@@ -538,17 +538,16 @@ def grad_norm(grads, stats: GradStats, max_norm: float = math.inf, grad_scale: f
 
 
 def clip_grads(grads, max_norm: float, stats: GradStats, out=None, grad_scale: float = 1.0, stream=None) -> torch.Tensor:
-    """grad_norm, then hashgrid_clip_grads: the gradients times stats.factor, in place or into the tensors of `out` (of the same
+    """hashgrid_clip_grads: grad_norm, and the gradients times stats.factor, in place or into the tensors of `out` (of the same
     types and sizes); gradients that are not all finite become zeros.  They keep their loss scale.  Returns stats.norm, as
     it was before.  (adam_steps clips on its way and needs grad_norm alone.)"""
     g = _grad_list(grads)
     to = None if out is None else _grad_list(out)
     if to is not None and to._kinds != g._kinds:
         raise HashGridError("out must be tensors of the gradients' types and sizes")
-    norm = grad_norm(g, stats, max_norm, grad_scale, stream)
-    _check(load_library().hashgrid_clip_grads(len(g), g._array, None if to is None else to._pointers, _stats_ptr(stats),
-                                              _stream_ptr(stream)), "hashgrid_clip_grads")
-    return norm
+    _check(load_library().hashgrid_clip_grads(len(g), g._array, None if to is None else to._pointers, grad_scale, max_norm,
+                                              _stats_ptr(stats), _stream_ptr(stream)), "hashgrid_clip_grads")
+    return stats.norm
 
 
 @dataclass

@@ -2,84 +2,125 @@
 // gradient norm, clipping, the optimiser step).
 //
 // The arrays' descriptions travel by value in the kernel's arguments, so that a call neither copies nor allocates device
-// memory and can be recorded into a graph.  The arrays are cut into units of kUnit scalars, numbered through all arrays of the
-// list, and every workgroup takes an equal run of them: arrays of any sizes, one scalar or 2^32 and more, give workgroups the
-// same work to within a unit.  Scalars are read and written 16 bytes a lane wherever the array starts: global loads and
-// stores of this target need no more than the element's own alignment.
+// memory and can be recorded into a graph.  The arrays are cut into units of some thousand scalars, numbered through all arrays of
+// the list, and dealt out to the workgroups in turn: arrays of any sizes, one scalar or 2^32 and more, give workgroups the same
+// work to within a unit, and what the chip reads at a time lies together (in turn 2.94 ms, a run of its own for each workgroup
+// 2.99: norm and optimiser step on 408 M fp32 scalars, before the other steps that the kernels name).  Scalars are read and
+// written 16 bytes a lane wherever the array starts: global loads and stores of this target need no more than the
+// element's own alignment.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "hashgrid.h"
 
 namespace hg {
 
 constexpr int kListThreads = 256;
-constexpr uint32_t kUnit = 2048;  // scalars: 8 a thread, one 16-byte access of a 16-bit type, two of fp32
+// Scalars a unit: 8 a thread where that gives every compute unit work, 32 a thread, several loads on their way at a time, where
+// there is enough of it.
+constexpr uint32_t kSmallUnit = 2048, kLargeUnit = 8192;
+constexpr uint32_t kWaveUnit = 1024;  // where a team is one wave: 16 a lane
+constexpr uint32_t kMaxListGroups = 2048;  // eight workgroups a compute unit
 
 // N descriptions of type Item (with members n and first: scalars, and the first unit)
 template <typename Item, int N>
 struct TensorList {
   static constexpr int kMost = N;
   uint32_t n_items;
-  uint32_t units;          // of all items together
-  uint32_t per, longer;    // a workgroup's units: per + 1 for the first `longer` of them, per for the others
+  uint32_t units;  // of all items together
+  uint32_t unit;   // scalars of one
   Item item[N];
 };
 
-// Calls f(item, begin, end) for every stretch of scalars that is this workgroup's.
-template <typename Item, int N, typename Fn>
-__device__ __forceinline__ void for_spans(const TensorList<Item, N>& list, Fn&& f) {
-  const uint32_t b = blockIdx.x;
-  uint32_t u = b * list.per + (b < list.longer ? b : list.longer);
-  const uint32_t end = u + list.per + (b < list.longer ? 1u : 0u);
-  if (u >= end) return;
-  // the item of unit u: as many items as start at or before it, less one; each lane looks at one of 64
-  uint32_t i = 0;
+// A team's way through its stretches of scalars: units first, first + teams, ...; a team is a workgroup, or one of its waves.
+//   for (Spans at(list, first, teams); at.within(list); at.advance()) ... list.item[at.i], scalars at.begin .. at.end-1
+// (The kernels' loops are written out with it: a function that took their bodies as a lambda made the compiler copy the list
+// from the arguments to every thread's private memory as soon as the body kept anything from one stretch to the next.)
+struct Spans {
+  uint32_t u, teams, i, next;
+  uint64_t begin, end;
+
+  template <typename List>
+  __device__ __forceinline__ Spans(const List& list, const uint32_t first, const uint32_t n_teams) : u(first), teams(n_teams) {
+    // the item of unit u: as many items as start at or before it, less one; each lane looks at one of 64
+    uint32_t before = 0;
 #pragma unroll
-  for (int at = 0; at < N; at += 64) {
-    const uint32_t k = at + (threadIdx.x & 63);
-    i += __popcll(__ballot(k < list.n_items && list.item[k < N ? k : N - 1].first <= u));
+    for (int at = 0; at < List::kMost; at += 64) {
+      const uint32_t k = at + (threadIdx.x & 63);
+      before += __popcll(__ballot(k < list.n_items && list.item[k < List::kMost ? k : 0].first <= u));
+    }
+    before = __builtin_amdgcn_readfirstlane(before);
+    i = before ? before - 1 : 0;
+    next = i + 1 < list.n_items ? list.item[i + 1].first : list.units;
   }
-  i = __builtin_amdgcn_readfirstlane(i) - 1;
-  while (u < end) {
-    const Item& it = list.item[i];
-    const uint32_t next = i + 1 < list.n_items ? list.item[i + 1].first : list.units;
-    const uint32_t stop = end < next ? end : next;
-    const uint64_t from = (uint64_t)(u - it.first) * kUnit, to = (uint64_t)(stop - it.first) * kUnit;
-    f(it, from, to < it.n ? to : it.n);
-    u = stop;
-    ++i;
+  template <typename List>
+  __device__ __forceinline__ bool within(const List& list) {
+    if (u >= list.units) return false;
+    while (u >= next) {
+      ++i;
+      next = i + 1 < list.n_items ? list.item[i + 1].first : list.units;
+    }
+    begin = (uint64_t)(u - list.item[i].first) * list.unit;
+    end = begin + list.unit < list.item[i].n ? begin + list.unit : list.item[i].n;
+    return true;
   }
-}
+  __device__ __forceinline__ void advance() { u += teams; }
+};
 
-// Workgroups for a list of `units`: two thousand, eight a compute unit, keep the memory busy; fewer where there is less.
-constexpr uint32_t kMaxListGroups = 2048;
-template <typename List>
-uint32_t deal_out(List& list) {
-  const uint32_t groups = list.units < kMaxListGroups ? (list.units ? list.units : 1) : kMaxListGroups;
-  list.per = list.units / groups;
-  list.longer = list.units % groups;
-  return groups;
-}
+inline uint64_t units_of(uint64_t n, uint32_t unit) { return n / unit + (n % unit != 0); }
 
-inline uint64_t units_of(uint64_t n) { return n / kUnit + (n % kUnit != 0); }
+// Large units from 8 M scalars on, where they still make a thousand (norm of 408 M fp16 scalars 145 us with large units and 183
+// with small ones, of 3 M fp16 and 9 M bf16 scalars in 204 tensors 18 and 33, of 12 M fp32 ones 15 and 18; clipping 5 M scalars in
+// 43 tensors 19 with either).
+inline uint32_t unit_for(uint64_t scalars) { return scalars > (8u << 20) ? kLargeUnit : kSmallUnit; }
+
+// Whether a list's gradients are too many for the last-level cache to hold from the norm's reading to the next: both then
+// pass by the caches.  (Measured on either side: norm and optimiser step on 408 M fp32 gradients, 1.6 GB, 2525 us passing by and
+// 2608 through the caches, on 58 M, 232 MB, 353 and 320, on 12 M 81 and 75.)
+constexpr uint64_t kCacheBytes = 256u << 20;
+
+inline uint32_t groups_of(uint32_t units) { return units < kMaxListGroups ? (units ? units : 1) : kMaxListGroups; }
 
 inline uint32_t dtype_bytes(uint32_t dtype) { return dtype == HG_F32 ? 4 : 2; }
 
-// V scalars of type T at any address that T may have
+// V scalars of type T at any address that T may have.  STREAM: nothing will read them again soon (non-temporal).
 template <typename T, int V>
-struct __attribute__((packed, aligned(sizeof(T)))) Vec {
-  T v[V];
+struct VecOf {
+  typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 };
 template <typename T, int V>
+struct Vec {
+  T v[V];
+};
+template <typename T, int V, bool STREAM>
 __device__ __forceinline__ Vec<T, V> load_vec(const T* p) {
-  return *reinterpret_cast<const Vec<T, V>*>(p);
+  const auto* at = reinterpret_cast<const typename VecOf<T, V>::type*>(p);
+  if constexpr (STREAM)
+    return __builtin_bit_cast(Vec<T, V>, __builtin_nontemporal_load(at));
+  else
+    return __builtin_bit_cast(Vec<T, V>, *at);
 }
+// Every store here is of that kind (clipping 58 M fp16 scalars into other arrays 75 -> 63 us, norm and step on 408 M 3.46 -> 3.00 ms).
 template <typename T, int V>
 __device__ __forceinline__ void store_vec(T* p, const Vec<T, V>& v) {
-  *reinterpret_cast<Vec<T, V>*>(p) = v;
+  __builtin_nontemporal_store(__builtin_bit_cast(typename VecOf<T, V>::type, v), reinterpret_cast<typename VecOf<T, V>::type*>(p));
+}
+
+// Calls f(first, std::integral_constant<int, K>) for vectors first, first + T, ... (K of them), over vectors 0 .. n-1 for the T
+// threads of a team: K = kAhead as long as all threads have that many, so that the loads in f stand side by side with no
+// branch between them (behind one the compiler waits for each), then what is left.
+template <int kAhead, int T, typename Fn>
+__device__ __forceinline__ void for_vectors(const uint32_t n, const uint32_t thread, Fn&& f) {
+  uint32_t q = 0;
+  for (; q + kAhead * T <= n; q += kAhead * T) f(q + thread, std::integral_constant<int, kAhead>{});
+  if (q + 2 * T <= n) {
+    f(q + thread, std::integral_constant<int, 2>{});
+    q += 2 * T;
+  }
+  for (q += thread; q < n; q += T) f(q, std::integral_constant<int, 1>{});
 }
 
 // Calls f with a null pointer of the C++ type behind an hg_dtype.

@@ -26,7 +26,7 @@ def adam(*rows, **kw):
 
 def test_the_structures_are_the_header_s():
     assert ctypes.sizeof(binding.hashgrid_grad) == 24 and ctypes.sizeof(binding.hashgrid_adam_tensor) == 80
-    assert binding.HG_GRAD_STATS_BYTES == 8 * 4 + 8 * 2048
+    assert binding.HG_GRAD_STATS_BYTES == 128 + 33 * 128 + 8 * 2048
 
 
 def test_grad_norm_status_codes():
@@ -49,21 +49,23 @@ def test_grad_norm_status_codes():
 
 
 def test_clip_grads_status_codes():
-    clip = binding.load_library().hashgrid_clip_grads
+    call = binding.load_library().hashgrid_clip_grads
+    clip = lambda n, g, out, stats, scale=1.0, bound=1.0: call(n, g, out, scale, bound, stats, None)
     pointers = lambda *p: (ctypes.c_void_p * len(p))(*p)
     two = grads((A, 64, 0), (A + 256, 64, 0))
-    assert clip(2, two, None, None, None) == 1
-    assert clip(2, two, None, A + 4, None) == 1
-    assert clip(2, two, pointers(None, A + 4096), A, None) == 1
-    assert clip(2, two, pointers(A + 4096, A + 8190), A, None) == 1
-    assert clip(2, grads((A, 64, 0), (A + 252, 64, 0)), None, A, None) == 1        # one scalar shared
-    assert clip(2, grads((A, 64, 0), (A, 64, 0)), None, A, None) == 1
-    assert clip(2, two, pointers(A + 4096, A + 4096 + 252), A, None) == 1
-    assert clip(2, two, pointers(A + 256, A), A, None) == 1                        # each into the other
-    assert clip(1, grads((A, 64, 1)), pointers(A + 2), A, None) == 1               # into itself, moved by one
+    assert clip(2, two, None, None) == 1
+    assert clip(2, two, None, A + 4) == 1
+    assert clip(2, two, pointers(None, A + 4096), A) == 1
+    assert clip(2, two, pointers(A + 4096, A + 8190), A) == 1
+    assert clip(2, grads((A, 64, 0), (A + 252, 64, 0)), None, A) == 1        # one scalar shared
+    assert clip(2, grads((A, 64, 0), (A, 64, 0)), None, A) == 1
+    assert clip(2, two, pointers(A + 4096, A + 4096 + 252), A) == 1
+    assert clip(2, two, pointers(A + 256, A), A) == 1                        # each into the other
+    assert clip(1, grads((A, 64, 1)), pointers(A + 2), A) == 1               # into itself, moved by one
     many = [(A + 0x1000 * i, 64, 2) for i in range(1023, -1, -1)]                  # in falling order, the last one twice
-    assert clip(1024, grads(*many[:-1], many[0]), None, A, None) == 1
-    assert clip(0, None, None, A, None) == 0 and clip(1, grads((None, 0, 0)), None, A, None) == 0
+    assert clip(1024, grads(*many[:-1], many[0]), None, A) == 1
+    assert clip(2, two, None, A, scale=0.0) == 1 and clip(2, two, None, A, bound=-1.0) == 1 and clip(2, two, None, A, bound=math.nan) == 1
+    assert clip(1025, grads(*[(A, 64, 0)] * 1025), None, A) == 2
 
 
 def test_adam_steps_status_codes():
