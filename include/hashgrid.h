@@ -467,6 +467,20 @@ typedef struct {
 hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam_tensor* tensors, float grad_scale, int zero_grad,
                               uint32_t step, hashgrid_grad_stats* stats, void* stream);
 
+/* hashgrid_train_step with the gradients of tables and weights together clipped by their norm between the backward passes and the
+ * optimiser: what hashgrid_grad_norm and hashgrid_adam_steps leave that are called there.  Where factor is 1 the results are
+ * hashgrid_train_step's; where a gradient is not finite tables and weights stay as they are and the step does not count.
+ *   max_norm  >= 0, may be infinity; in units of the MEAN loss's gradient, over B * n_out scalars and without loss_scale (which
+ *             must be positive here): a bound that means the same for every batch size and loss scale.  The L2 term of
+ *             weights_adam.l2_reg is added after clipping and is not part of the norm.
+ *   stats     holds the norm and the number of the optimiser step, 1 with the first call on zeroed memory
+ *   grads     n_entries * F scalars and as many as `weights` behind them, fp32, device, 16-byte aligned, scratch
+ * B == 0 is HG_OK and changes nothing. */
+hg_status hashgrid_train_step_clipped(const hashgrid_t* hg, const hashgrid_train_state* st, float max_norm,
+                                      hashgrid_grad_stats* stats, float* grads, uint32_t B, const float* x,
+                                      const float* target, void* y, void* dLdy, void* workspace, uint64_t workspace_bytes,
+                                      void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* hashgrid_strerror(hg_status s);
 

@@ -40,7 +40,7 @@ EXPORTS = ("hashgrid_create", "hashgrid_destroy", "hashgrid_n_entries", "hashgri
            "hashgrid_encode_mlp_fwd", "hashgrid_encode_bwd_static", "hashgrid_encode_mlp_fwd_train", "hashgrid_mlp_bwd",
            "hashgrid_adam_step_half_grad", "hashgrid_loss_grad", "hashgrid_mlp_fwd",
            "hashgrid_encode_mlp_bwd_input", "hashgrid_train_step", "hashgrid_grad_norm", "hashgrid_clip_grads",
-           "hashgrid_adam_steps")
+           "hashgrid_adam_steps", "hashgrid_train_step_clipped")
 PROBE_EXPORTS = ("hashgrid_probe_copy", "hashgrid_probe_gather", "hashgrid_probe_atomic_add",
                  "hashgrid_probe_gather_lines")
 
@@ -138,6 +138,9 @@ def load_library() -> ctypes.CDLL:
     lib.hashgrid_encode_mlp_bwd_input.restype = ctypes.c_int
     lib.hashgrid_train_step.argtypes = [vp, ctypes.POINTER(hashgrid_train_state), u32, vp, vp, vp, vp, vp, u64, u32, vp]
     lib.hashgrid_train_step.restype = ctypes.c_int
+    lib.hashgrid_train_step_clipped.argtypes = [vp, ctypes.POINTER(hashgrid_train_state), ctypes.c_float, vp, vp, u32, vp, vp, vp, vp,
+                                                vp, u64, vp]
+    lib.hashgrid_train_step_clipped.restype = ctypes.c_int
     lib.hashgrid_grad_norm.argtypes = [u32, vp, ctypes.c_float, ctypes.c_float, vp, vp]
     lib.hashgrid_grad_norm.restype = ctypes.c_int
     lib.hashgrid_clip_grads.argtypes = [u32, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp]
@@ -399,18 +402,27 @@ class HashGrid:
         return dLdx
 
     def train_step(self, state: hashgrid_train_state, x: torch.Tensor, target: torch.Tensor, y: torch.Tensor,
-                   dLdy: torch.Tensor, step: int, stream=None) -> None:
+                   dLdy: torch.Tensor, step: int, stream=None, clip=None) -> None:
         """hashgrid_train_step; the scratch of the sorted backward pass is one kept on this object.  The pointers in
-        `state` are the caller's to check (HashGridModel does)."""
+        `state` are the caller's to check (HashGridModel does).  clip: (max_norm, GradStats, fp32 scratch for
+        the gradients of tables and weights) for hashgrid_train_step_clipped, which counts the steps itself (`step` is not
+        looked at)."""
         B, sp = x.shape[0], _stream_ptr(stream)
         arrays = (_dev(x, torch.float32, (B, self.d), "x"), _dev(target, torch.float32, (B, state.n_out), "target"),
                   _dev(y, torch.float16, (B, self.L * self.F), "y"), _dev(dLdy, torch.float16, (B, self.L * self.F), "dLdy"))
         self._counted = None
         _, pays, need = self._of_batch(B)
         ws = self._workspace(need, x.device, stream, sp) if pays and need else None
-        _check(self._lib.hashgrid_train_step(self._h, ctypes.byref(state), B, *arrays,
-                                             None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), step, sp),
-               "hashgrid_train_step")
+        scratch = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
+        if clip is None:
+            _check(self._lib.hashgrid_train_step(self._h, ctypes.byref(state), B, *arrays, *scratch, step, sp),
+                   "hashgrid_train_step")
+        else:
+            max_norm, stats, grads = clip
+            n = self.n_entries * self.F + 64 * (self.L * self.F + 64 + state.n_out)
+            _check(self._lib.hashgrid_train_step_clipped(self._h, ctypes.byref(state), max_norm, _stats_ptr(stats),
+                                                         _dev(grads, torch.float32, (n,), "scratch of the gradients"), B, *arrays,
+                                                         *scratch, sp), "hashgrid_train_step_clipped")
 
     def debug_count_outside(self, x: torch.Tensor, stream=None) -> int:
         """hashgrid_debug_count_outside: coordinates of x that are not in [0,1) (synchronises)."""

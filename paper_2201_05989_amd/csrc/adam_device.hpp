@@ -67,7 +67,7 @@ struct SideJob {
   uint32_t blocks;
   SumLayout at;
   AdamArgs a;
-  AdamState w;         // the weights, in the order of SumLayout::scalar_of
+  AdamState w;         // the weights, in the order of SumLayout::scalar_of; m null: p32 takes their gradients, and Adam is left out
   const float4* sums;  // [n_parts][quads][64]
   const double* loss_parts;
   uint32_t n_parts;
@@ -96,7 +96,9 @@ __device__ __forceinline__ void run_side_job(const SideJob& job, const uint32_t 
 #pragma unroll
     for (uint32_t s = 0; s < kSegments; ++s) g += reinterpret_cast<const float*>(part + s * 64 + lane)[t];
     const int i = job.at.scalar_of((int)quad, (int)t, (int)lane);
-    if (i >= 0) {
+    if (i >= 0 && !job.w.m) {
+      job.w.p32[i] = g;
+    } else if (i >= 0) {
       float p = job.w.p32[i];
       g = job.a.l2 != 0.0f ? fmaf(job.a.l2, p, g) : g;
       if (g != 0.0f) {

@@ -1419,8 +1419,9 @@ static void launch_scan(const hashgrid* h, const Workspace& ws, uint32_t zero_ma
   else launch(std::integral_constant<int, 0>{}, b32);
 }
 
-// The optimiser's part of a sorted backward pass (launch_binned_adam)
+// The optimiser's part of a sorted backward pass (launch_binned_adam); without `adam` (launch_binned_job) only the side job
 struct BinnedAdam {
+  bool adam;
   AdamArgs a;
   AdamState st;
   SideJob job;
@@ -1561,7 +1562,7 @@ static hg_status launch_binned(const hashgrid* h, uint32_t B, const float* x, co
                        ws.records, ws.item_counters, n_queues, g, overwrite_mask, NoAdam{});
   };
   if constexpr (kAdam) {
-    if (ba) {
+    if (ba && ba->adam) {
       AdamOut out;
       out.a = ba->a;
       out.st = ba->st;
@@ -1606,16 +1607,12 @@ static hg_status launch_binned_f(const hashgrid* h, uint32_t B, const float* x, 
   }
 }
 
-hg_status launch_binned_adam(const hashgrid* h, uint32_t B, const float* x, const void* dy, float* zeros, void* workspace,
-                             bool counted, const AdamArgs& a, const AdamState& st, const SideJob& job, hipStream_t s) {
+static hg_status launch_binned_ba(const hashgrid* h, uint32_t B, const float* x, const void* dy, float* grad, void* workspace,
+                                  bool counted, bool overwrite, const BinnedAdam& ba, hipStream_t s) {
   if (h->bp.corner_records || h->cfg.io_dtype != HG_F16 || h->cfg.grad_dtype != HG_F32) return HG_ERR_UNSUPPORTED;
   Workspace ws;
   carve(h, B, static_cast<uint8_t*>(workspace), &ws);
-  BinnedAdam ba;
-  ba.a = a;
-  ba.st = st;
-  ba.job = job;
-#define HG_BA(D, F) launch_binned<D, _Float16, F, false>(h, B, x, dy, zeros, ws, counted, false, s, &ba)
+#define HG_BA(D, F) launch_binned<D, _Float16, F, false>(h, B, x, dy, grad, ws, counted, overwrite, s, &ba)
   switch (h->cfg.d * 16 + h->cfg.F) {
     case 2 * 16 + 1: return HG_BA(2, 1);
     case 2 * 16 + 2: return HG_BA(2, 2);
@@ -1628,6 +1625,16 @@ hg_status launch_binned_adam(const hashgrid* h, uint32_t B, const float* x, cons
     default: return HG_ERR_UNSUPPORTED;
   }
 #undef HG_BA
+}
+
+hg_status launch_binned_adam(const hashgrid* h, uint32_t B, const float* x, const void* dy, float* zeros, void* workspace,
+                             bool counted, const AdamArgs& a, const AdamState& st, const SideJob& job, hipStream_t s) {
+  return launch_binned_ba(h, B, x, dy, zeros, workspace, counted, false, BinnedAdam{true, a, st, job}, s);
+}
+
+hg_status launch_binned_job(const hashgrid* h, uint32_t B, const float* x, const void* dy, float* grad, void* workspace,
+                            bool counted, const SideJob& job, hipStream_t s) {
+  return launch_binned_ba(h, B, x, dy, grad, workspace, counted, true, BinnedAdam{false, AdamArgs{}, AdamState{}, job}, s);
 }
 
 template <typename IT>

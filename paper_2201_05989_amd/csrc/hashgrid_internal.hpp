@@ -65,6 +65,9 @@ hg_status launch_mlp_train(uint32_t B, uint32_t n_in, uint32_t n_out, const void
 // zero, and are again after the call: where several workgroups share a chunk their sums meet there.
 hg_status launch_binned_adam(const hashgrid* h, uint32_t B, const float* x, const void* dy, float* zeros, void* workspace,
                              bool counted, const AdamArgs& a, const AdamState& st, const SideJob& job, hipStream_t s);
+// the same without the optimiser: grad is written in full (HG_BWD_OVERWRITE), and the job rides along
+hg_status launch_binned_job(const hashgrid* h, uint32_t B, const float* x, const void* dy, float* grad, void* workspace,
+                            bool counted, const SideJob& job, hipStream_t s);
 // hashgrid.hip: the optimiser's step on the entries that the batch's corners reach (d = 2 or 3); grad is all zeros after it
 hg_status launch_adam_touched(const hashgrid* h, uint32_t B, const float* x, float* grad, const AdamArgs& a,
                               const AdamState& st, const SideJob& job, hipStream_t s);

@@ -13,7 +13,7 @@ import math
 
 import torch
 
-from .binding import (_LOSSES, HG_TRAIN_SCRATCH_BYTES, HashGrid, HashGridError, _dev, hashgrid_adam_config,
+from .binding import (_LOSSES, HG_TRAIN_SCRATCH_BYTES, GradStats, HashGrid, HashGridError, _dev, hashgrid_adam_config,
                       hashgrid_train_state)
 
 N_HIDDEN = 64
@@ -22,11 +22,14 @@ N_HIDDEN = 64
 class HashGridModel:
     def __init__(self, d: int, n_out: int, L: int = 16, F: int = 2, T: int = 1 << 19, N_min: int = 16, N_max: int = 2048,
                  loss: str = "l2", lr: float = 1e-2, l2_reg: float = 1e-6, loss_scale: float = 1.0, seed: int = 0,
-                 interp: int = 0):
+                 interp: int = 0, max_grad_norm: float | None = None):
         """loss: "l2" or "mape".  The paper's loss is a mean over the batch; what travels backward here is the gradient
         of the summed loss times loss_scale, because the network's backward pass rounds dL/dout to half precision
         and 1/n would push it into the subnormals.  Adam is indifferent to a common factor of all gradients, and
-        the L2 term of the weights gets the same factor (n * loss_scale), so the update is the mean loss's."""
+        the L2 term of the weights gets the same factor (n * loss_scale), so the update is the mean loss's.
+        max_grad_norm: the largest norm that the mean loss's gradient over all tables and weights may have: a larger one is
+        scaled down to it before the optimiser's step (infinity: never, the norm is only taken), and a step whose gradient is
+        not finite is left out.  grad_stats then holds the norm and the steps that were taken.  None: neither."""
         self.grid = HashGrid(d, L, F, T, N_min, N_max, "f16", "f16", interp)
         self.d, self.n_in, self.n_out = d, L * F, n_out
         self.loss, self.lr, self.l2_reg, self.loss_scale = loss, lr, l2_reg, loss_scale
@@ -50,6 +53,25 @@ class HashGridModel:
             weights_adam=hashgrid_adam_config(0.0, 0.9, 0.99, 1e-15, 0.0), loss_sum=self._loss_sum.data_ptr(),
             scratch=self._scratch.data_ptr())
         self._buf_B = 0
+        self._max_grad_norm = self.grad_stats = self._grads = None
+        self.max_grad_norm = max_grad_norm
+
+    @property
+    def max_grad_norm(self) -> float | None:
+        return self._max_grad_norm
+
+    @max_grad_norm.setter
+    def max_grad_norm(self, bound: float | None) -> None:
+        """May be changed between steps (outside a captured one: the bound is part of the capture)."""
+        if bound is not None:
+            if not bound >= 0:
+                raise HashGridError(f"max_grad_norm must be None or at least 0, not {bound!r}")
+            if self.grad_stats is None:
+                self.grad_stats = GradStats()
+                self._grads = torch.empty(self.tables.numel() + self._n_weights, device="cuda")
+            if self._max_grad_norm is None:  # the device counts on from the steps that were taken without it
+                self.grad_stats.steps.fill_(self.steps)
+        self._max_grad_norm = bound
 
     def _views(self, flat):
         out, at = [], 0
@@ -108,7 +130,8 @@ class HashGridModel:
         synchronises; last_loss() does."""
         B = x.shape[0]
         self._buffers(B)
-        self.grid.train_step(self._train_state(B), x, target, self._y, self._dy, self.steps + 1)
+        clip = None if self._max_grad_norm is None else (self._max_grad_norm, self.grad_stats, self._grads)
+        self.grid.train_step(self._train_state(B), x, target, self._y, self._dy, self.steps + 1, clip=clip)
         self.steps += 1
         self._n_last = B * self.n_out
 

@@ -1,0 +1,205 @@
+"""hashgrid_train_step_clipped (HashGridModel(max_grad_norm=...)) against hashgrid_train_step where nothing is clipped, and against the
+single calls that it stands for, in a loop as a user's program writes it.
+
+Where nothing rounds (small integer tables, points at vertices, dyadic slopes) sums are the same in any order, what the optimiser
+gets is the same bits, and so is what it leaves: all comparisons are exact, but for the norm, which is held to the rounding of
+its result (2^-24), and the replays, which see sums in another order from their second step on and are held to what one model
+trained twice may differ by.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import grad_norm_oracle as gno
+from paper_2201_05989_amd import (AdamList, AdamTensor, GradStats, HashGridError, HashGridModel, adam_steps, binding, grad_norm, loss_grad,
+                                  mlp_bwd)
+
+pytestmark = pytest.mark.gpu
+
+
+def exact_model(seed, d=3, L=8, F=2, T=1 << 14, n_out=1, loss="l2", interp=0, bound=None):
+    m = HashGridModel(d, n_out, L=L, F=F, T=T, N_min=4, N_max=512, loss=loss, seed=seed, interp=interp, max_grad_norm=bound)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    m.tables.copy_(torch.randint(-1, 2, m.tables.shape, device="cuda", generator=gen))
+    m.tables_half.copy_(m.tables)
+    W = torch.randint(-1, 2, m.weights.shape, device="cuda", generator=gen).float()
+    m.weights.copy_(W * (torch.rand(m.weights.shape, device="cuda", generator=gen) < 0.2))
+    m.weights_half.copy_(m.weights)
+    return m, gen
+
+
+def exact_batch(m, B, gen):
+    x = (torch.randint(0, 4, (B, m.d), device="cuda", generator=gen).float() / 4).contiguous()
+    p = m.infer(x)
+    if m.loss == "l2":
+        return x, (p - torch.randint(-4, 5, p.shape, device="cuda", generator=gen) / 8.0).contiguous()
+    return x, torch.where(torch.rand(p.shape, device="cuda", generator=gen) < 0.5, 0.99, -0.99).float().contiguous()
+
+
+def state_of(m):
+    return {"tables": m.tables, "tables_half": m.tables_half, "m": m._tab_m, "v": m._tab_v, "weights": m.weights,
+            "weights_half": m.weights_half, "weights m": m._net_m, "weights v": m._net_v}
+
+
+CASES = [dict(B=1), dict(B=777, F=4, n_out=3, interp=1), dict(B=2049, d=2, F=8, T=1 << 19, n_out=9, loss="mape"), dict(B=40000, T=1 << 12, loss="mape"),
+         dict(B=100003, T=1 << 16, n_out=32), dict(B=30000, F=8, T=1 << 15, n_out=17, interp=1), dict(B=70001, d=2, F=4, T=1 << 15, n_out=2)]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "B%d-F%d" % (c["B"], c.get("F", 2)))
+def test_a_bound_that_nothing_reaches_changes_nothing(case):
+    kw = {k: v for k, v in case.items() if k != "B"}
+    a, gen = exact_model(5, **kw)
+    b, _ = exact_model(5, bound=float("inf"), **kw)
+    x, target = exact_batch(a, case["B"], gen)
+    a.step(x, target)
+    b.step(x, target)
+    for name, t in state_of(a).items():
+        assert torch.equal(t, state_of(b)[name]), name
+    assert not b._tab_zeros.any() and int(b.grad_stats.steps) == 1 and float(b.grad_stats.factor) == 1.0
+    assert abs(a.last_loss() - b.last_loss()) <= 1e-12 * abs(a.last_loss())
+
+
+def single_calls(m, x, target, B, stats, model, grad, dw, bound):
+    """A clipped iteration as a program of its own writes it."""
+    y = torch.empty((B, m.n_in), dtype=torch.float16, device="cuda")
+    dy, out = torch.empty_like(y), torch.empty((B, m.n_out), device="cuda")
+    dout = torch.empty_like(out)
+    W = m._network()
+    m.grid.encode_mlp_fwd(x, m.tables_half, *W, out, y=y)
+    loss_grad(out, target, m.loss, m.loss_scale, dout)
+    dw.zero_()
+    mlp_bwd(y, *W, dout, dy, *m._views(dw))
+    m.grid.encode_bwd(x, dy, grad, overwrite=True)
+    grad_norm(model.grads, stats, bound, grad_scale=1.0 / (m.loss_scale * B * m.n_out))
+    adam_steps(model, stats, zero_grad=False)
+
+
+@pytest.mark.parametrize("case", CASES[1:], ids=lambda c: "B%d-F%d" % (c["B"], c.get("F", 2)))
+def test_clipped_steps_are_those_of_the_single_calls(case):
+    kw = {k: v for k, v in case.items() if k != "B"}
+    B = case["B"]
+    probe, gen = exact_model(9, bound=float("inf"), **kw)
+    x, target = exact_batch(probe, B, gen)
+    probe.step(x, target)
+    bound = 0.25 * float(probe.grad_stats.norm)
+    assert bound > 0
+    a, _ = exact_model(9, bound=bound, **kw)
+    b, _ = exact_model(9, **kw)
+    grad, dw, stats = torch.zeros_like(b.tables), torch.zeros_like(b.weights), GradStats()
+    l2 = b.l2_reg * b.loss_scale * (B * b.n_out)
+    model = AdamList([AdamTensor(b.tables, grad, b._tab_m, b._tab_v, b.tables_half, lr=b.lr),
+                      AdamTensor(b.weights, dw, b._net_m, b._net_v, b.weights_half, lr=b.lr, l2_reg=l2)])
+    a.step(x, target)
+    single_calls(b, x, target, B, stats, model, grad, dw, bound)
+    # the norm's units: the mean loss, whatever the batch
+    want = gno.norm([grad.cpu().double().numpy(), dw.cpu().double().numpy()], np.float32(1.0 / (B * b.n_out)))
+    assert abs(float(stats.norm) - want) <= 2.0 ** -24 * 1.001 * want
+    assert torch.equal(a.grad_stats.memory[:16], stats.memory[:16]) and 0.2 < float(stats.factor) < 0.3
+    for name, t in state_of(a).items():
+        assert torch.equal(t, state_of(b)[name]), name
+    assert not a._tab_zeros.any()
+    assert float(a._net_m.abs().sum()) > 0 or B == 1
+
+
+@pytest.mark.parametrize("B", [300, 40000])
+def test_a_batch_that_is_not_finite_leaves_the_model_as_it_was(B):
+    m = HashGridModel(3, 2, L=8, T=1 << 14, N_max=512, max_grad_norm=1.0, seed=1)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.rand((B, 3), device="cuda", generator=gen).clamp_(max=1 - 2.0 ** -24)
+    good = torch.randn((B, 2), device="cuda", generator=gen)
+    bad = good.clone()
+    bad[B // 2, 1] = float("nan")
+    m.step(x, good)
+    before = {k: v.clone() for k, v in state_of(m).items()}
+    m.step(x, bad)
+    assert not np.isfinite(float(m.grad_stats.norm)) and int(m.grad_stats.steps) == 1
+    for name, t in state_of(m).items():
+        assert torch.equal(t, before[name]), name
+    assert not m._tab_zeros.any()
+    m.step(x, good)
+    assert np.isfinite(float(m.grad_stats.norm)) and int(m.grad_stats.steps) == 2 and not torch.equal(m.tables, before["tables"])
+    assert all(bool(torch.isfinite(t).all()) for t in state_of(m).values())
+
+
+@pytest.mark.parametrize("B", [300, 40000])
+def test_a_captured_step_counts_on(B):
+    """Replays of one recorded step against a model that takes the same steps one by one, eager work in between."""
+    a, gen = exact_model(3, n_out=2, bound=1e-4)
+    b, _ = exact_model(3, n_out=2, bound=1e-4)
+    x, target = exact_batch(a, B, gen)
+    a.step(x, target)  # buffers and workspace are there
+    b.step(x, target)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):  # the stream's own workspace, too
+        a.step(x, target)
+    b.step(x, target)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        a.step(x, target)
+    for i in range(4):
+        nx, nt = exact_batch(b, B, gen)
+        x.copy_(nx)
+        target.copy_(nt)
+        graph.replay()
+        torch.cuda.synchronize()
+        b.step(x, target)
+        torch.randn(1000, device="cuda").sum().item()
+        assert int(a.grad_stats.steps) == int(b.grad_stats.steps) == 3 + i
+        # after the first update nothing is exact any more: sums in another order, fp32
+        assert abs(float(a.grad_stats.norm) - float(b.grad_stats.norm)) <= 1e-2 * float(b.grad_stats.norm)
+        assert float(a.grad_stats.norm) > 0 and not a._tab_zeros.any()
+
+
+def test_the_bound_may_be_changed_between_steps():
+    m, gen = exact_model(4)
+    with pytest.raises(HashGridError):
+        m.max_grad_norm = -1.0
+    with pytest.raises(HashGridError):
+        m.max_grad_norm = float("nan")
+    assert m.max_grad_norm is None and m.grad_stats is None
+    x, target = exact_batch(m, 2000, gen)
+    for _ in range(3):
+        m.step(x, target)
+    m.max_grad_norm = 1e-3
+    m.step(x, target)
+    assert int(m.grad_stats.steps) == 4 and m.steps == 4
+    before = m.tables.clone()
+    m.max_grad_norm = 0.0      # no gradient but the L2 term's
+    m.step(x, target)
+    assert int(m.grad_stats.steps) == 5 and float(m.grad_stats.factor) == 0.0 and torch.equal(m.tables, before)
+    m.max_grad_norm = None
+    m.step(x, target)
+    assert int(m.grad_stats.steps) == 5 and m.steps == 6
+    m.max_grad_norm = 1.0
+    m.step(x, target)
+    assert int(m.grad_stats.steps) == 7 == m.steps
+
+
+def test_status_codes_and_an_empty_batch():
+    m, gen = exact_model(4, bound=1.0)
+    x, target = exact_batch(m, 500, gen)
+    m.step(x, target)
+    before = {k: v.clone() for k, v in state_of(m).items()}
+    lib, st = m.grid._lib, m._train_state(500)
+    stats, scratch = m.grad_stats.memory.data_ptr(), m._grads.data_ptr()
+    call = lambda st, bound, stats, scratch, B=500: lib.hashgrid_train_step_clipped(
+        m.grid._h, ctypes.byref(st), bound, stats, scratch, B, x.data_ptr(), target.data_ptr(), m._y.data_ptr(), m._dy.data_ptr(), None, 0, None)
+    assert call(st, -1.0, stats, scratch) == 1 and call(st, float("nan"), stats, scratch) == 1
+    assert call(st, 1.0, None, scratch) == 1 and call(st, 1.0, stats + 4, scratch) == 1
+    assert call(st, 1.0, stats, None) == 1 and call(st, 1.0, stats, scratch + 2) == 1
+    for scale in (0.0, -1.0, 1e-45):  # (the last one's reciprocal is beyond fp32)
+        st.loss_scale = scale
+        assert call(st, 1.0, stats, scratch) == 1
+    st = m._train_state(500)
+    assert call(st, 1.0, stats, scratch, 0) == 0
+    torch.cuda.synchronize()
+    assert int(m.grad_stats.steps) == 1 and all(torch.equal(t, before[k]) for k, t in state_of(m).items())
+    with pytest.raises(HashGridError):
+        m.grid.train_step(st, x, target, m._y, m._dy, 1, clip=(1.0, torch.zeros(4, device="cuda"), m._grads))
+    with pytest.raises(HashGridError):
+        m.grid.train_step(st, x, target, m._y, m._dy, 1, clip=(1.0, m.grad_stats, m._grads[1:]))
+    assert binding.HG_GRAD_STATS_BYTES == m.grad_stats.memory.numel()
