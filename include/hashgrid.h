@@ -455,7 +455,7 @@ typedef struct {
   uint32_t reserved;    /* 0 */
 } hashgrid_adam_tensor;
 
-/* hashgrid_adam_step on every tensor of the list, in one launch for every three dozen of them.  The gradient that the step takes is
+/* hashgrid_adam_step on every tensor of the list, in one launch for every four dozen of them.  The gradient that the step takes is
  * grad * (grad_scale * factor), in fp32, plus cfg.l2_reg * value; scalars for which that is exactly 0 are passed over.
  *   tensors  [n_tensors]  HOST array, read during the call
  *   stats    NULL: factor 1, and the step's number is `step` >= 1.

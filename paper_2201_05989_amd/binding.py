@@ -486,9 +486,12 @@ class GradStats:
 
     def __init__(self, device=None):
         self.memory = torch.zeros(HG_GRAD_STATS_BYTES, dtype=torch.uint8, device="cuda" if device is None else device)
+        if not self.memory.is_cuda:
+            raise HashGridError("GradStats are device memory")
         word = [self.memory[4 * i:4 * i + 4] for i in range(4)]
         self.norm, self.factor = word[0].view(torch.float32), word[1].view(torch.float32)
         self.step, self.steps = word[2].view(torch.int32), word[3].view(torch.int32)
+        self._device = self.memory.get_device()
 
 
 def _on_current_device(device, what: str) -> None:
@@ -499,8 +502,18 @@ def _on_current_device(device, what: str) -> None:
 def _stats_ptr(stats) -> int:
     if not isinstance(stats, GradStats):
         raise HashGridError("stats must be a GradStats")
-    _on_current_device(stats.memory.get_device(), "stats")
+    _on_current_device(stats._device, "stats")
     return stats.memory.data_ptr()
+
+
+def _one_device(tensors):
+    devices = {t.get_device() for t in tensors}
+    if len(devices) > 1:
+        raise HashGridError("the tensors of a list must be on one device")
+    return devices.pop() if devices else None
+
+
+_data_ptr = torch.Tensor.data_ptr
 
 
 class GradList:
@@ -512,22 +525,18 @@ class GradList:
         self._look_up()
 
     def _look_up(self):
-        devices = set()
         for i, t in enumerate(self.tensors):
             if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype in _LIST_DTYPES):
                 raise HashGridError(f"tensor {i} of the list must be a contiguous fp32, fp16 or bf16 device tensor")
-            devices.add(t.get_device())
-        if len(devices) > 1:
-            raise HashGridError("the tensors of a list must be on one device")
-        self._device = devices.pop() if devices else None
-        self._at = [t.data_ptr() for t in self.tensors]
+        self._device = _one_device(self.tensors)
         self._kinds = [(t.dtype, t.numel()) for t in self.tensors]
-        self._pointers = (ctypes.c_void_p * len(self._at))(*self._at)
-        self._array = (hashgrid_grad * len(self._at))(*[(at, n, _LIST_DTYPES[dtype], 0)
-                                                        for at, (dtype, n) in zip(self._at, self._kinds)])
+        at = [t.data_ptr() for t in self.tensors]
+        self._pointers = (ctypes.c_void_p * len(at))(*at)
+        self._array = (hashgrid_grad * len(at))(*[(p, n, _LIST_DTYPES[dtype], 0) for p, (dtype, n) in zip(at, self._kinds)])
+        self._at = at
 
     def _current(self):
-        if [t.data_ptr() for t in self.tensors] != self._at:
+        if list(map(_data_ptr, self.tensors)) != self._at:
             self._look_up()
         _on_current_device(self._device, "tensors")
         return self
@@ -537,7 +546,7 @@ class GradList:
 
 
 def _grad_list(grads) -> GradList:
-    return (grads if isinstance(grads, GradList) else GradList(grads))._current()
+    return grads._current() if isinstance(grads, GradList) else GradList(grads)._current()
 
 
 def grad_norm(grads, stats: GradStats, max_norm: float = math.inf, grad_scale: float = 1.0, stream=None) -> torch.Tensor:
@@ -555,8 +564,8 @@ def clip_grads(grads, max_norm: float, stats: GradStats, out=None, grad_scale: f
     it was before.  (adam_steps clips on its way and needs grad_norm alone.)"""
     g = _grad_list(grads)
     to = None if out is None else _grad_list(out)
-    if to is not None and to._kinds != g._kinds:
-        raise HashGridError("out must be tensors of the gradients' types and sizes")
+    if to is not None and (to._kinds != g._kinds or to._device != g._device):
+        raise HashGridError("out must be tensors of the gradients' types and sizes, on their device")
     _check(load_library().hashgrid_clip_grads(len(g), g._array, None if to is None else to._pointers, grad_scale, max_norm,
                                               _stats_ptr(stats), _stream_ptr(stream)), "hashgrid_clip_grads")
     return stats.norm
@@ -565,7 +574,7 @@ def clip_grads(grads, max_norm: float, stats: GradStats, out=None, grad_scale: f
 @dataclass
 class AdamTensor:
     """One tensor of adam_steps: fp32 master copy and moments, gradient (fp32, fp16 or bf16), 16-bit working copy or None, and
-    the hyper-parameters, which may be changed between steps."""
+    the hyper-parameters.  Any of them may be replaced between steps."""
     params_master: torch.Tensor
     grad: torch.Tensor
     m: torch.Tensor
@@ -577,10 +586,9 @@ class AdamTensor:
     eps: float = 1e-15
     l2_reg: float = 0.0
 
-    def _key(self):
-        h = self.params_half
-        return (self.params_master.data_ptr(), None if h is None else h.data_ptr(), self.grad.data_ptr(), self.m.data_ptr(),
-                self.v.data_ptr(), self.lr, self.beta1, self.beta2, self.eps, self.l2_reg)
+    def __setattr__(self, name, value):
+        self.__dict__[name] = value
+        self.__dict__["_changes"] = self.__dict__.get("_changes", 0) + 1  # (what an AdamList goes by)
 
 
 class AdamList:
@@ -589,42 +597,41 @@ class AdamList:
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
-        self._grads = None
         self._look_up()
 
     def _look_up(self):
-        devices, rows = set(), []
+        rows, flat = [], []
         for i, t in enumerate(self.tensors):
             n = t.grad.numel()
-            for name, a, types in (("params_master", t.params_master, (torch.float32,)), ("m", t.m, (torch.float32,)),
-                                   ("v", t.v, (torch.float32,)), ("grad", t.grad, tuple(_LIST_DTYPES)),
-                                   ("params_half", t.params_half, (torch.float16, torch.bfloat16))):
+            for name, types in (("params_master", (torch.float32,)), ("params_half", (torch.float16, torch.bfloat16)),
+                                ("grad", tuple(_LIST_DTYPES)), ("m", (torch.float32,)), ("v", (torch.float32,))):
+                a = getattr(t, name)
                 if name == "params_half" and a is None:
                     continue
                 if not (a.is_cuda and a.is_contiguous() and a.dtype in types and a.numel() == n):
                     raise HashGridError(f"{name} of tensor {i} must be a contiguous device tensor of {n} scalars, {types}")
-                devices.add(a.get_device())
-            half = HG_F16 if t.params_half is None else _LIST_DTYPES[t.params_half.dtype]
-            key = t._key()
-            rows.append((*key[:5], n, _LIST_DTYPES[t.grad.dtype], half, hashgrid_adam_config(*key[5:]), 0))
-        if len(devices) > 1:
-            raise HashGridError("the tensors of a list must be on one device")
-        self._device = devices.pop() if devices else None
-        self._keys = [t._key() for t in self.tensors]
-        self._array = (hashgrid_adam_tensor * len(rows))(*rows)
+                flat.append(a)
+            h = t.params_half
+            rows.append((t.params_master.data_ptr(), None if h is None else h.data_ptr(), t.grad.data_ptr(), t.m.data_ptr(),
+                         t.v.data_ptr(), n, _LIST_DTYPES[t.grad.dtype], HG_F16 if h is None else _LIST_DTYPES[h.dtype],
+                         hashgrid_adam_config(t.lr, t.beta1, t.beta2, t.eps, t.l2_reg), 0))
+        self._device = _one_device(flat)
+        self._flat, self._array = flat, (hashgrid_adam_tensor * len(rows))(*rows)
+        self._grads = GradList([t.grad for t in self.tensors])
+        self._at = list(map(_data_ptr, flat))
+        self._changes = [t._changes for t in self.tensors]
 
     def _current(self):
-        if [t._key() for t in self.tensors] != self._keys:
+        if [t._changes for t in self.tensors] != self._changes or list(map(_data_ptr, self._flat)) != self._at:
             self._look_up()
         _on_current_device(self._device, "tensors")
         return self
 
     @property
     def grads(self) -> GradList:
-        known = self._grads
-        if known is None or any(t.grad is not g for t, g in zip(self.tensors, known.tensors)):
-            known = self._grads = GradList([t.grad for t in self.tensors])
-        return known
+        if [t._changes for t in self.tensors] != self._changes:
+            self._look_up()
+        return self._grads
 
     def __len__(self):
         return len(self.tensors)
@@ -635,7 +642,7 @@ def adam_steps(tensors, stats: GradStats | None = None, step: int = 0, zero_grad
     """hashgrid_adam_steps on an AdamList or any sequence of AdamTensor: adam_step on all of them in one launch.  With
     stats, after grad_norm over the same gradients: they are clipped on the way, the step is left out where one of them is not
     finite, and the device counts the steps.  Without: the step's number is `step`, counted from 1."""
-    a = (tensors if isinstance(tensors, AdamList) else AdamList(tensors))._current()
+    a = tensors._current() if isinstance(tensors, AdamList) else AdamList(tensors)._current()
     _check(load_library().hashgrid_adam_steps(len(a), a._array, grad_scale, int(zero_grad), step,
                                               None if stats is None else _stats_ptr(stats), _stream_ptr(stream)),
            "hashgrid_adam_steps")

@@ -23,12 +23,11 @@ namespace {
 struct AdamItem {
   AdamState st;  // (p16: 16-bit copy of either type)
   void* grad;
-  uint64_t n;
-  uint32_t first, grad_dtype, copy_dtype;
+  Place at;
   AdamArgs a;  // (inv_c1, inv_sqrt_c2: of the caller's step, where the device does not count)
 };
-using AdamList = TensorList<AdamItem, 36>;
-static_assert(sizeof(AdamList) <= 3840, "with the other arguments at most 4 KB");
+using AdamList = TensorList<AdamItem, 48>;
+static_assert(sizeof(AdamList) <= 4000, "with the other arguments at most 4 KB");
 
 // beta^t by repeated squaring: 2 log2(t) roundings of 64 bits
 __device__ __forceinline__ double power(double beta, uint32_t t) {
@@ -104,7 +103,7 @@ __device__ __forceinline__ void step_span(const AdamItem& it, const AdamArgs& a,
   void* const grad = it.grad;
   void* const copy = it.st.p16;
   float *const p = it.st.p32, *const m = it.st.m, *const v = it.st.v;
-  const uint32_t n = (uint32_t)(end - begin), n4 = n / 4, gt = it.grad_dtype, ct = it.copy_dtype;
+  const uint32_t n = (uint32_t)(end - begin), n4 = n / 4, gt = it.at.dtype, ct = it.at.copy_dtype;
   // (two or eight vectors ahead instead of four: 78 and 79 us for 75 on 12 M scalars, norm included)
   for_vectors<4, kListThreads>(n4, threadIdx.x, [&](const uint32_t q0, auto many) __attribute__((always_inline)) {
     constexpr int K = decltype(many)::value;
@@ -243,17 +242,16 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool once = bytes > hg::kCacheBytes;
   hg::AdamList list;
-  list.unit = hg::unit_for(scalars);
+  list.unit = hg::step_unit_for(scalars);
   uint32_t i = 0;
   do {  // (once for an empty list too where the device counts the steps)
     list.n_items = list.units = 0;
     for (; i < n_tensors && list.n_items < (uint32_t)hg::AdamList::kMost; ++i) {
       const hashgrid_adam_tensor& t = tensors[i];
       if (t.n_scalars == 0) continue;
-      list.item[list.n_items++] = hg::AdamItem{hg::AdamState{t.params_master, static_cast<_Float16*>(t.params_half), t.m, t.v}, t.grad,
-                                               t.n_scalars, list.units, t.grad_dtype, t.half_dtype,
-                                               hg::adam_args(t.cfg, step ? step : 1u)};
-      list.units += (uint32_t)hg::units_of(t.n_scalars, list.unit);
+      list.item[list.n_items++] =
+          hg::AdamItem{hg::AdamState{t.params_master, static_cast<_Float16*>(t.params_half), t.m, t.v}, t.grad,
+                       hg::next_place(list, t.n_scalars, t.grad_dtype, t.half_dtype & 15), hg::adam_args(t.cfg, step ? step : 1u)};
     }
     if (list.n_items == 0 && n_ranges) break;
     const uint32_t groups = hg::groups_of(list.units);

@@ -37,18 +37,17 @@ namespace {
 
 struct NormItem {
   const void* data;
-  uint64_t n;
-  uint32_t first, dtype;
+  Place at;
 };
-using NormList = TensorList<NormItem, 128>;
+using NormList = TensorList<NormItem, 240>;
 
 struct ClipItem {
   const void* data;
   void* out;
-  uint64_t n;
-  uint32_t first, dtype;
+  Place at;
 };
-using ClipList = TensorList<ClipItem, 64>;
+using ClipList = TensorList<ClipItem, 160>;
+static_assert(sizeof(NormList) <= 4000 && sizeof(ClipList) <= 4000, "with the other arguments at most 4 KB");
 
 // Squares of scalars [begin, end): the share of one of a team's THREADS threads.
 template <bool STREAM, int THREADS, typename T>
@@ -129,7 +128,7 @@ __global__ __launch_bounds__(kListThreads) void norm(const NormList list, hashgr
   double sum = 0.0;
   for (Spans at(list, blockIdx.x, gridDim.x); at.within(list); at.advance()) {
     const NormItem& it = list.item[at.i];
-    with_type(it.dtype, [&](auto* t) __attribute__((always_inline)) {
+    with_type(it.at.dtype, [&](auto* t) __attribute__((always_inline)) {
       using T = std::remove_pointer_t<decltype(t)>;
       sum += sum_squares<STREAM, kListThreads>(static_cast<const T*>(it.data), at.begin, at.end, threadIdx.x);
     });
@@ -193,7 +192,7 @@ __global__ __launch_bounds__(kListThreads) void clip(const ClipList list, const 
   for (Spans at(list, blockIdx.x, gridDim.x); at.within(list); at.advance()) {
     const ClipItem& it = list.item[at.i];
     if (factor == 1.0f && it.data == it.out) continue;  // in place, nothing to clip
-    with_type(it.dtype, [&](auto* t) __attribute__((always_inline)) {
+    with_type(it.at.dtype, [&](auto* t) __attribute__((always_inline)) {
       using T = std::remove_pointer_t<decltype(t)>;
       scale_span<kListThreads>(static_cast<const T*>(it.data), static_cast<T*>(it.out), factor, at.begin, at.end, threadIdx.x);
     });
@@ -212,7 +211,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_list(const ClipList list,
   double sum = 0.0;
   for (Spans at(list, wave, kSmallThreads / 64); at.within(list); at.advance()) {
     const ClipItem& it = list.item[at.i];
-    with_type(it.dtype, [&](auto* t) __attribute__((always_inline)) {
+    with_type(it.at.dtype, [&](auto* t) __attribute__((always_inline)) {
       using T = std::remove_pointer_t<decltype(t)>;
       sum += sum_squares<false, 64>(static_cast<const T*>(it.data), at.begin, at.end, lane);
     });
@@ -225,7 +224,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_list(const ClipList list,
   for (Spans at(list, wave, kSmallThreads / 64); at.within(list); at.advance()) {
     const ClipItem& it = list.item[at.i];
     if (factor == 1.0f && it.data == it.out) continue;
-    with_type(it.dtype, [&](auto* t) __attribute__((always_inline)) {
+    with_type(it.at.dtype, [&](auto* t) __attribute__((always_inline)) {
       using T = std::remove_pointer_t<decltype(t)>;
       scale_span<64>(static_cast<const T*>(it.data), static_cast<T*>(it.out), factor, at.begin, at.end, lane);
     });
@@ -258,17 +257,14 @@ void take(List& list, uint32_t& i, const uint32_t n_tensors, const hashgrid_grad
   list.n_items = list.units = 0;
   for (; i < n_tensors && list.n_items < (uint32_t)List::kMost; ++i) {
     if (grads[i].n_scalars == 0) continue;
-    list.item[list.n_items++] = make(i, list.units);
-    list.units += (uint32_t)units_of(grads[i].n_scalars, list.unit);
+    list.item[list.n_items++] = make(i, next_place(list, grads[i].n_scalars, grads[i].dtype));
   }
 }
 
 // The norm, and clipping (`clipped`) into `out` or in place; arguments checked.
 hg_status launch(uint32_t n_tensors, const hashgrid_grad* grads, const bool clipped, void* const* out, const uint64_t scalars,
                  const uint64_t bytes, const float grad_scale, const float max_norm, hashgrid_grad_stats* stats, hipStream_t s) {
-  auto clip_item = [&](const uint32_t i, const uint32_t first) {
-    return ClipItem{grads[i].data, out ? out[i] : grads[i].data, grads[i].n_scalars, first, grads[i].dtype};
-  };
+  auto clip_item = [&](const uint32_t i, const Place& at) { return ClipItem{grads[i].data, out ? out[i] : grads[i].data, at}; };
   constexpr uint32_t kWaves = kSmallThreads / 64;
   uint64_t small_units = 0;
   for (uint32_t i = 0; i < n_tensors && small_units <= kWaves; ++i) small_units += units_of(grads[i].n_scalars, kWaveUnit);
@@ -284,9 +280,7 @@ hg_status launch(uint32_t n_tensors, const hashgrid_grad* grads, const bool clip
   norms.unit = unit_for(scalars);
   uint32_t i = 0, prior = 0;
   while (i < n_tensors) {
-    take(norms, i, n_tensors, grads, [&](const uint32_t k, const uint32_t first) {
-      return NormItem{grads[k].data, grads[k].n_scalars, first, grads[k].dtype};
-    });
+    take(norms, i, n_tensors, grads, [&](const uint32_t k, const Place& at) { return NormItem{grads[k].data, at}; });
     const uint32_t now = groups_of(norms.units), all = now > prior ? now : prior;
     hipLaunchKernelGGL(bytes > kCacheBytes ? norm<true> : norm<false>, dim3(now), dim3(kListThreads), 0, s, norms, stats, prior,
                        i < n_tensors ? 0u : all, grad_scale, max_norm);

@@ -19,13 +19,19 @@
 namespace hg {
 
 constexpr int kListThreads = 256;
-// Scalars a unit: 8 a thread where that gives every compute unit work, 32 a thread, several loads on their way at a time, where
-// there is enough of it.
+// Scalars a unit: from 8 a thread, which give the most workgroups something to do, to 32, several loads on their way at a time.
 constexpr uint32_t kSmallUnit = 2048, kLargeUnit = 8192;
 constexpr uint32_t kWaveUnit = 1024;  // where a team is one wave: 16 a lane
 constexpr uint32_t kMaxListGroups = 2048;  // eight workgroups a compute unit
 
-// N descriptions of type Item (with members n and first: scalars, and the first unit)
+// What every description of an array begins its place in the list with: its first unit, and the scalars of its last one (the
+// others are full), with the types beside them.  Short, because 4 KB of arguments hold the list.
+struct Place {
+  uint32_t first;
+  uint32_t last : 16, dtype : 4, copy_dtype : 4;
+};
+
+// N descriptions of type Item, with a Place `at`
 template <typename Item, int N>
 struct TensorList {
   static constexpr int kMost = N;
@@ -47,35 +53,61 @@ struct Spans {
   __device__ __forceinline__ Spans(const List& list, const uint32_t first, const uint32_t n_teams) : u(first), teams(n_teams) {
     // the item of unit u: as many items as start at or before it, less one; each lane looks at one of 64
     uint32_t before = 0;
+    auto look = [&](const uint32_t k) __attribute__((always_inline)) {
+      before += __popcll(__ballot(k < list.n_items && list.item[k < List::kMost ? k : 0].at.first <= u));
+    };
+    look(threadIdx.x & 63);
+    if (list.n_items > 64) {  // (short lists are not to wait for arguments that they do not use)
 #pragma unroll
-    for (int at = 0; at < List::kMost; at += 64) {
-      const uint32_t k = at + (threadIdx.x & 63);
-      before += __popcll(__ballot(k < list.n_items && list.item[k < List::kMost ? k : 0].first <= u));
+      for (int at = 64; at < List::kMost; at += 64) look(at + (threadIdx.x & 63));
     }
     before = __builtin_amdgcn_readfirstlane(before);
     i = before ? before - 1 : 0;
-    next = i + 1 < list.n_items ? list.item[i + 1].first : list.units;
+    next = end_of(list, i);
   }
   template <typename List>
   __device__ __forceinline__ bool within(const List& list) {
     if (u >= list.units) return false;
     while (u >= next) {
       ++i;
-      next = i + 1 < list.n_items ? list.item[i + 1].first : list.units;
+      next = end_of(list, i);
     }
-    begin = (uint64_t)(u - list.item[i].first) * list.unit;
-    end = begin + list.unit < list.item[i].n ? begin + list.unit : list.item[i].n;
+    begin = (uint64_t)(u - list.item[i].at.first) * list.unit;
+    end = begin + (u + 1 == next ? list.item[i].at.last : list.unit);
     return true;
+  }
+  template <typename List>
+  static __device__ __forceinline__ uint32_t end_of(const List& list, const uint32_t i) {
+    return i + 1 < list.n_items ? list.item[i + 1].at.first : list.units;
   }
   __device__ __forceinline__ void advance() { u += teams; }
 };
 
 inline uint64_t units_of(uint64_t n, uint32_t unit) { return n / unit + (n % unit != 0); }
 
-// Large units from 8 M scalars on, where they still make a thousand (norm of 408 M fp16 scalars 145 us with large units and 183
-// with small ones, of 3 M fp16 and 9 M bf16 scalars in 204 tensors 18 and 33, of 12 M fp32 ones 15 and 18; clipping 5 M scalars in
-// 43 tensors 19 with either).
-inline uint32_t unit_for(uint64_t scalars) { return scalars > (8u << 20) ? kLargeUnit : kSmallUnit; }
+// The place of the next array of the list, of n > 0 scalars.
+template <typename List>
+Place next_place(List& list, uint64_t n, uint32_t dtype, uint32_t copy_dtype = 0) {
+  Place at;
+  at.first = list.units;
+  at.last = (uint32_t)((n - 1) % list.unit) + 1;
+  at.dtype = dtype;
+  at.copy_dtype = copy_dtype;
+  list.units += (uint32_t)units_of(n, list.unit);
+  return at;
+}
+
+// Scalars a unit for a list of so many.  Norm and clipping: the smallest unit with which every workgroup has one at the most, and
+// the large one beyond that (4.5 M fp32 scalars: norm 8.6 us with units of 4096 and 10.6 with 2048, clipped 13.2 and 15.1;
+// 12 M 14.8 with 8192, 16.3 with 6144 and 17.2 with 2048; 408 M fp16 145 with 8192 and 183 with 2048).
+inline uint32_t unit_for(uint64_t scalars) {
+  uint32_t unit = kSmallUnit;
+  while (unit < kLargeUnit && scalars > (uint64_t)unit * kMaxListGroups) unit *= 2;
+  return unit;
+}
+// The optimiser step, with four arrays to a scalar, fills the memory with small units for longer (norm and step on 6 M scalars 41.6
+// us with 2048 and 43.3 with 4096, 408 M 2.94 ms with 8192 and 3.2 with 2048).
+inline uint32_t step_unit_for(uint64_t scalars) { return scalars > (8u << 20) ? kLargeUnit : kSmallUnit; }
 
 // Whether a list's gradients are too many for the last-level cache to hold from the norm's reading to the next: both then
 // pass by the caches.  (Measured on either side: norm and optimiser step on 408 M fp32 gradients, 1.6 GB, 2525 us passing by and
