@@ -401,7 +401,7 @@ hg_status hashgrid_train_step(const hashgrid_t* hg, const hashgrid_train_state* 
 #define HG_BF16 2u                           /* beside HG_F32 and HG_F16, in the lists below only */
 #define HG_MAX_TENSORS 1024u                 /* tensors a call; more returns HG_ERR_UNSUPPORTED */
 #define HG_MAX_TENSOR_SCALARS (1ull << 42)   /* scalars a tensor, and all tensors of a call together */
-#define HG_GRAD_NORM_GROUPS 2048u
+#define HG_GRAD_NORM_GROUPS 1024u
 #define HG_GRAD_NORM_GATES 33u
 
 typedef struct {

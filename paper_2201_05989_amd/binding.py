@@ -26,7 +26,7 @@ HG_ERR_UNSUPPORTED = 2
 HG_STATIC_SCRATCH_BYTES = 64 << 20
 HG_LOSS_L2, HG_LOSS_MAPE = 0, 1
 HG_TRAIN_SCRATCH_BYTES = 256 * (8 + 40 * 1024)
-HG_GRAD_STATS_BYTES = 128 + 33 * 128 + 2048 * 8
+HG_GRAD_STATS_BYTES = 128 + 33 * 128 + 1024 * 8
 _LOSSES = {"l2": HG_LOSS_L2, "mape": HG_LOSS_MAPE, HG_LOSS_L2: HG_LOSS_L2, HG_LOSS_MAPE: HG_LOSS_MAPE}
 
 _DTYPES = {"f32": HG_F32, "f16": HG_F16, torch.float32: HG_F32, torch.float16: HG_F16}

@@ -47,6 +47,7 @@ struct ClipItem {
   Place at;
 };
 using ClipList = TensorList<ClipItem, 160>;
+static_assert(kMaxListGroups <= HG_GRAD_NORM_GROUPS, "a place for every workgroup's sum");
 static_assert(sizeof(NormList) <= 4000 && sizeof(ClipList) <= 4000, "with the other arguments at most 4 KB");
 
 // Squares of scalars [begin, end): the share of one of a team's THREADS threads.
@@ -103,7 +104,7 @@ __device__ __forceinline__ float write_norm(hashgrid_grad_stats* st, const doubl
 }
 
 // Whether this workgroup is the last of the launch to come here, in thread 0.  Two levels: a counter serves one addition after
-// the other, and 2048 on one word would queue up for longer than the sums take.
+// the other, and a thousand on one word would queue up for longer than the sums take.
 __device__ __forceinline__ bool last_to_arrive(uint32_t (*arrived)[32]) {
   constexpr uint32_t kGates = HG_GRAD_NORM_GATES - 1;
   auto last_of = [](uint32_t* counter, const uint32_t n) {

@@ -22,7 +22,10 @@ constexpr int kListThreads = 256;
 // Scalars a unit: from 8 a thread, which give the most workgroups something to do, to 32, several loads on their way at a time.
 constexpr uint32_t kSmallUnit = 2048, kLargeUnit = 8192;
 constexpr uint32_t kWaveUnit = 1024;  // where a team is one wave: 16 a lane
-constexpr uint32_t kMaxListGroups = 2048;  // eight workgroups a compute unit
+// Workgroups at most, four a compute unit: as many as run at a time in the optimiser step, whose four vectors ahead take the
+// registers.  Norm and clipping, of which more fit, read no faster with more (norm of 408 M fp16 scalars 122 us with 1024 and 129
+// with 2048, of 12 M fp32 13.5 and 14.1).
+constexpr uint32_t kMaxListGroups = 1024;
 
 // What every description of an array begins its place in the list with: its first unit, and the scalars of its last one (the
 // others are full), with the types beside them.  Short, because 4 KB of arguments hold the list.
@@ -50,35 +53,29 @@ struct Spans {
   uint64_t begin, end;
 
   template <typename List>
-  __device__ __forceinline__ Spans(const List& list, const uint32_t first, const uint32_t n_teams) : u(first), teams(n_teams) {
-    // the item of unit u: as many items as start at or before it, less one; each lane looks at one of 64
-    uint32_t before = 0;
-    auto look = [&](const uint32_t k) __attribute__((always_inline)) {
-      before += __popcll(__ballot(k < list.n_items && list.item[k < List::kMost ? k : 0].at.first <= u));
-    };
-    look(threadIdx.x & 63);
-    if (list.n_items > 64) {  // (short lists are not to wait for arguments that they do not use)
-#pragma unroll
-      for (int at = 64; at < List::kMost; at += 64) look(at + (threadIdx.x & 63));
-    }
-    before = __builtin_amdgcn_readfirstlane(before);
-    i = before ? before - 1 : 0;
-    next = end_of(list, i);
-  }
+  __device__ __forceinline__ Spans(const List& list, const uint32_t first, const uint32_t n_teams)
+      : u(first), teams(n_teams), i(0), next(0) {}
   template <typename List>
   __device__ __forceinline__ bool within(const List& list) {
     if (u >= list.units) return false;
-    while (u >= next) {
-      ++i;
-      next = end_of(list, i);
+    if (u >= next) {
+      // the item of unit u: as many items as start at or before it, less one; each lane looks at one of 64.  (Item by item a step
+      // over a hundred small tensors costs 10 us.)
+      uint32_t before = 0;
+      auto look = [&](const uint32_t k) __attribute__((always_inline)) {
+        before += __popcll(__ballot(k < list.n_items && list.item[k < List::kMost ? k : 0].at.first <= u));
+      };
+      look(threadIdx.x & 63);
+      if (list.n_items > 64) {  // (short lists are not to wait for arguments that they do not use)
+#pragma unroll
+        for (int at = 64; at < List::kMost; at += 64) look(at + (threadIdx.x & 63));
+      }
+      i = __builtin_amdgcn_readfirstlane(before) - 1;
+      next = i + 1 < list.n_items ? list.item[i + 1].at.first : list.units;
     }
     begin = (uint64_t)(u - list.item[i].at.first) * list.unit;
     end = begin + (u + 1 == next ? list.item[i].at.last : list.unit);
     return true;
-  }
-  template <typename List>
-  static __device__ __forceinline__ uint32_t end_of(const List& list, const uint32_t i) {
-    return i + 1 < list.n_items ? list.item[i + 1].at.first : list.units;
   }
   __device__ __forceinline__ void advance() { u += teams; }
 };
@@ -97,12 +94,12 @@ Place next_place(List& list, uint64_t n, uint32_t dtype, uint32_t copy_dtype = 0
   return at;
 }
 
-// Scalars a unit for a list of so many.  Norm and clipping: the smallest unit with which every workgroup has one at the most, and
-// the large one beyond that (4.5 M fp32 scalars: norm 8.6 us with units of 4096 and 10.6 with 2048, clipped 13.2 and 15.1;
+// Scalars a unit for a list of so many.  Norm and clipping: the smallest unit with which a workgroup has two at the most, and the
+// large one beyond that (4.5 M fp32 scalars: norm 8.6 us with units of 4096 and 10.6 with 2048, clipped 13.2 and 15.1;
 // 12 M 14.8 with 8192, 16.3 with 6144 and 17.2 with 2048; 408 M fp16 145 with 8192 and 183 with 2048).
 inline uint32_t unit_for(uint64_t scalars) {
   uint32_t unit = kSmallUnit;
-  while (unit < kLargeUnit && scalars > (uint64_t)unit * kMaxListGroups) unit *= 2;
+  while (unit < kLargeUnit && scalars > 2ull * unit * kMaxListGroups) unit *= 2;
   return unit;
 }
 // The optimiser step, with four arrays to a scalar, fills the memory with small units for longer (norm and step on 6 M scalars 41.6
@@ -114,7 +111,7 @@ inline uint32_t step_unit_for(uint64_t scalars) { return scalars > (8u << 20) ? 
 // 2608 through the caches, on 58 M, 232 MB, 353 and 320, on 12 M 81 and 75.)
 constexpr uint64_t kCacheBytes = 256u << 20;
 
-inline uint32_t groups_of(uint32_t units) { return units < kMaxListGroups ? (units ? units : 1) : kMaxListGroups; }
+inline uint32_t groups_of(uint32_t units, uint32_t most = kMaxListGroups) { return units < most ? (units ? units : 1) : most; }
 
 inline uint32_t dtype_bytes(uint32_t dtype) { return dtype == HG_F32 ? 4 : 2; }
 

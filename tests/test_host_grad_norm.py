@@ -26,7 +26,7 @@ def adam(*rows, **kw):
 
 def test_the_structures_are_the_header_s():
     assert ctypes.sizeof(binding.hashgrid_grad) == 24 and ctypes.sizeof(binding.hashgrid_adam_tensor) == 80
-    assert binding.HG_GRAD_STATS_BYTES == 128 + 33 * 128 + 8 * 2048
+    assert binding.HG_GRAD_STATS_BYTES == 128 + 33 * 128 + 8 * 1024
 
 
 def test_grad_norm_status_codes():
