@@ -482,7 +482,8 @@ class GradStats:
       factor  fp32 [1]   min(1, max_norm / norm); 0 where a gradient is not finite
       step    int32 [1]  number of the optimiser step that is due; 0 where it is left out because a gradient is not finite
       steps   int32 [1]  optimiser steps taken by adam_steps; set it (steps.fill_(n)) to resume
-    Views of device memory: reading one as a number waits for the stream."""
+    Views of device memory: reading one as a number waits for the stream.  Made (and cleared) on torch's current stream, so before
+    a capture and not within one."""
 
     def __init__(self, device=None):
         self.memory = torch.zeros(HG_GRAD_STATS_BYTES, dtype=torch.uint8, device="cuda" if device is None else device)
@@ -517,8 +518,8 @@ _data_ptr = torch.Tensor.data_ptr
 
 
 class GradList:
-    """Gradients of a model, of any shapes, fp32, fp16 and bf16 mixed, looked over once for many calls.  The tensors keep their
-    sizes and types; one whose memory has moved since the last call is looked up again."""
+    """Gradients of a model, at most 1024 tensors of any shapes, fp32, fp16 and bf16 mixed, looked over once for many calls.  The
+    tensors keep their sizes and types; one whose memory has moved since the last call is looked up again."""
 
     def __init__(self, grads):
         self.tensors = list(grads)
@@ -571,7 +572,7 @@ def clip_grads(grads, max_norm: float, stats: GradStats, out=None, grad_scale: f
     return stats.norm
 
 
-@dataclass
+@dataclass(eq=False)
 class AdamTensor:
     """One tensor of adam_steps: fp32 master copy and moments, gradient (fp32, fp16 or bf16), 16-bit working copy or None, and
     the hyper-parameters.  Any of them may be replaced between steps."""
@@ -602,13 +603,13 @@ class AdamList:
     def _look_up(self):
         rows, flat = [], []
         for i, t in enumerate(self.tensors):
-            n = t.grad.numel()
+            n = t.params_master.numel() if isinstance(t.params_master, torch.Tensor) else 0
             for name, types in (("params_master", (torch.float32,)), ("params_half", (torch.float16, torch.bfloat16)),
                                 ("grad", tuple(_LIST_DTYPES)), ("m", (torch.float32,)), ("v", (torch.float32,))):
                 a = getattr(t, name)
                 if name == "params_half" and a is None:
                     continue
-                if not (a.is_cuda and a.is_contiguous() and a.dtype in types and a.numel() == n):
+                if not (isinstance(a, torch.Tensor) and a.is_cuda and a.is_contiguous() and a.dtype in types and a.numel() == n):
                     raise HashGridError(f"{name} of tensor {i} must be a contiguous device tensor of {n} scalars, {types}")
                 flat.append(a)
             h = t.params_half

@@ -51,7 +51,9 @@ def check_norm(grads, stats, max_norm, grad_scale=1.0):
     assert step == int(stats.steps) + 1
 
 
-LISTS = [[1], [0], [], [2047], [2048], [2049], [0, 5, 0, 1], [7, 4096, 1, 1, 300, 65537], [100003, 3], [1] * 300, list(range(1, 140)),
+MANY = [k * 7919 % 40000 + 1 for k in range(300)]  # a second launch, and workgroups that go from one tensor to a far one
+
+LISTS = [MANY, [1], [0], [], [2047], [2048], [2049], [0, 5, 0, 1], [7, 4096, 1, 1, 300, 65537], [100003, 3], [1] * 300, list(range(1, 140)),
          [5_300_017, 11, 2049, 900_001]]
 
 
@@ -103,7 +105,7 @@ def test_no_gradient_is_too_large_or_too_small(value, kind):
     assert torch.equal(out, torch.zeros_like(g) if float(stats.factor) == 0 else (g.float() * stats.factor).to(g.dtype))
 
 
-CLIPS = [[1], [0, 3], [2049, 1, 7], [7, 4096, 1, 1, 300, 65537], [9] * 200, [3_000_001, 65]]
+CLIPS = [MANY, [1], [0, 3], [2049, 1, 7], [7, 4096, 1, 1, 300, 65537], [9] * 200, [3_000_001, 65]]
 
 
 @pytest.mark.parametrize("sizes", CLIPS, ids=lambda s: f"{len(s)}x{sum(s)}")
@@ -193,7 +195,7 @@ def tensors_for_adam(sizes, kinds, seed, shift, l2):
 
 ADAMS = [([1], ["f32"], 0), ([3, 4, 5], ["f32", "f16", "bf16"], 0), ([0, 2047, 2049, 1], ["bf16", "f32", "f16"], 1),
          ([100_003, 17, 5000], ["f32", "f16"], 0), ([100_003, 17, 5000], ["f16", "f32"], 3), (list(range(1, 120)), ["f32", "f16", "bf16"], 1),
-         ([2_500_001, 6208], ["f32"], 0)]
+         ([2_500_001, 6208], ["f32"], 0), (MANY[:100], ["bf16", "f32", "f16"], 1)]
 
 
 @pytest.mark.parametrize("sizes,kinds,shift", ADAMS, ids=lambda a: str(len(a)) if isinstance(a, list) else str(a))
@@ -389,7 +391,7 @@ def test_refusals():
     clip_grads([h[:20], h[20:40]], 1.0, stats, out=[h[:20], g[:20]])   # in place for one of them
     p, m, v = (torch.zeros(64, device="cuda") for _ in range(3))
     good = dict(params_master=p, grad=g, m=m, v=v)
-    for change in ({"grad": g[:32]}, {"m": m.half()}, {"v": v.cpu()}, {"params_half": p}, {"beta1": 1.0}, {"eps": -1.0}, {"l2_reg": float("inf")},
+    for change in ({"grad": None}, {"params_master": 1.0}, {"grad": g[:32]}, {"m": m.half()}, {"v": v.cpu()}, {"params_half": p}, {"beta1": 1.0}, {"eps": -1.0}, {"l2_reg": float("inf")},
                    {"v": m}, {"params_master": g}):
         with pytest.raises(HashGridError):
             adam_steps([AdamTensor(**{**good, **change})], step=1)
