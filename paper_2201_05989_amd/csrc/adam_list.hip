@@ -4,7 +4,7 @@
 // Memory bound, as the step on one array is (adam.hip): a scalar with a gradient costs 12 bytes of reads and 12 to 14 of writes
 // beside its gradient; the clipped gradient is never stored.  Scalars without a gradient keep every bit, but memory is read and
 // written by the line: where one of the 32 scalars that share a line of each fp32 array has a gradient, all of the line is
-// read, past the caches, and written back.  Left out lane by lane, the stores leave lines with holes behind, which
+// read and written back, past the caches where they do not hold it all from one step to the next.  Left out lane by lane, the stores leave lines with holes behind, which
 // cost the memory more than whole ones (norm and step, fp32 gradients: 58 M scalars of which 22 % have one 437 -> 321 us, 408 M
 // with 63 % 2.92 -> 2.61 ms, 12 M with 95 % 85 -> 75; lines passed by the caches and left out lane by lane 466, 3.80, 76).
 // Lines in which no scalar has a gradient cost their gradient's bytes.
@@ -96,8 +96,16 @@ __device__ __forceinline__ void store_copy(void* array, const uint32_t dtype, co
   }
 }
 
+// Which arrays are read past the caches.  kState: values and moments, where a step's arrays are more than kResidentBytes: beyond
+// that they do not survive until the next step (norm and step, three models in turn, of 4.5 M scalars, 81 MB each, 34.1 us past
+// the caches and 30.5 through them; 6 M, 108 MB, 41.5 and 41.9; 14 M, 252 MB, 83.7 and 93.7.  One model of 12 M, 220 MB, and
+// nothing else running, 75 and 71: in a training step, whose other passes need the caches, the same).
+// kAll: the gradients as well, where the norm has read them past the caches (kCacheBytes).
+enum class Reach { kNone, kState, kAll };
+constexpr uint64_t kResidentBytes = 96u << 20;
+
 // Scalars [begin, end) of one tensor.  taken: the step is taken; else only the gradient is cleared, where asked to.
-template <bool ZERO_GRAD, bool STREAM>
+template <bool ZERO_GRAD, Reach REACH>
 __device__ __forceinline__ void step_span(const AdamItem& it, const AdamArgs& a, const float scale, const bool taken, const uint64_t begin,
                                           const uint64_t end) {
   void* const grad = it.grad;
@@ -111,7 +119,7 @@ __device__ __forceinline__ void step_span(const AdamItem& it, const AdamArgs& a,
     Vec<float, 4> g[K], pp[K], mm[K], vv[K];
     bool any[K], run[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) bits[k] = load_bits<STREAM>(grad, gt, begin + (q0 + k * kListThreads) * 4);
+    for (int k = 0; k < K; ++k) bits[k] = load_bits<REACH == Reach::kAll>(grad, gt, begin + (q0 + k * kListThreads) * 4);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const uint64_t at = begin + (q0 + k * kListThreads) * 4;
@@ -122,9 +130,9 @@ __device__ __forceinline__ void step_span(const AdamItem& it, const AdamArgs& a,
       const bool near = (__ballot(any[k]) >> (threadIdx.x & 56) & 0xff) != 0;  // eight lanes: a cache line of each fp32 array
       run[k] = taken && (near || a.l2 != 0.0f);
       if (run[k]) {
-        pp[k] = load_vec<float, 4, true>(p + at);
-        mm[k] = load_vec<float, 4, true>(m + at);
-        vv[k] = load_vec<float, 4, true>(v + at);
+        pp[k] = load_vec<float, 4, REACH != Reach::kNone>(p + at);
+        mm[k] = load_vec<float, 4, REACH != Reach::kNone>(m + at);
+        vv[k] = load_vec<float, 4, REACH != Reach::kNone>(v + at);
       }
     }
 #pragma unroll
@@ -171,7 +179,7 @@ __device__ __forceinline__ void step_span(const AdamItem& it, const AdamArgs& a,
   }
 }
 
-template <bool ZERO_GRAD, bool STREAM>
+template <bool ZERO_GRAD, Reach REACH>
 __global__ __launch_bounds__(kListThreads) void adam_list(const AdamList list, const float grad_scale,
                                                           hashgrid_grad_stats* __restrict__ stats) {
   // every workgroup reads `step`, one writes `steps`: no workgroup reads what another writes
@@ -198,9 +206,14 @@ __global__ __launch_bounds__(kListThreads) void adam_list(const AdamList list, c
       a.inv_c1 = inv_c1;
       a.inv_sqrt_c2 = inv_sqrt_c2;
     }
-    step_span<ZERO_GRAD, STREAM>(it, a, scale, step != 0, at.begin, at.end);
+    step_span<ZERO_GRAD, REACH>(it, a, scale, step != 0, at.begin, at.end);
   }
 }
+
+using StepKernel = void (*)(AdamList, float, hashgrid_grad_stats*);
+const StepKernel kernels[2][3] = {
+    {adam_list<false, Reach::kNone>, adam_list<false, Reach::kState>, adam_list<false, Reach::kAll>},
+    {adam_list<true, Reach::kNone>, adam_list<true, Reach::kState>, adam_list<true, Reach::kAll>}};
 
 bool misaligned(const void* p, uint32_t bytes) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
 
@@ -240,7 +253,9 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
   if (n_ranges == 0 && !stats) return HG_OK;
   if (hg::ranges_clash(ranges, n_ranges)) return HG_ERR_INVALID_ARG;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const bool once = bytes > hg::kCacheBytes;
+  const hg::Reach reach = bytes > hg::kCacheBytes                           ? hg::Reach::kAll
+                          : bytes + 14 * scalars > hg::kResidentBytes ? hg::Reach::kState
+                                                                      : hg::Reach::kNone;
   // Half as many workgroups where that still leaves each some ten units: with fewer streams open the memory is faster (norm and
   // step on 58 M scalars 305 us with 512 and 320 with 1024, on 12 M 74.3 and 73.5, on 7 M 48.7 and 46.5).
   const uint32_t most = scalars > (32u << 20) ? hg::kMaxListGroups / 2 : hg::kMaxListGroups;
@@ -258,8 +273,7 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
     }
     if (list.n_items == 0 && n_ranges) break;
     const uint32_t groups = hg::groups_of(list.units, most);
-    const auto kernel = zero_grad ? (once ? hg::adam_list<true, true> : hg::adam_list<true, false>)
-                                  : (once ? hg::adam_list<false, true> : hg::adam_list<false, false>);
+    const auto kernel = hg::kernels[zero_grad ? 1 : 0][(int)reach];
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(hg::kListThreads), 0, s, list, grad_scale, stats);
   } while (i < n_tensors);
   return hipGetLastError() == hipSuccess ? HG_OK : HG_ERR_DEVICE;

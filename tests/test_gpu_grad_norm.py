@@ -195,7 +195,7 @@ def tensors_for_adam(sizes, kinds, seed, shift, l2):
 
 ADAMS = [([1], ["f32"], 0), ([3, 4, 5], ["f32", "f16", "bf16"], 0), ([0, 2047, 2049, 1], ["bf16", "f32", "f16"], 1),
          ([100_003, 17, 5000], ["f32", "f16"], 0), ([100_003, 17, 5000], ["f16", "f32"], 3), (list(range(1, 120)), ["f32", "f16", "bf16"], 1),
-         ([2_500_001, 6208], ["f32"], 0), (MANY[:100], ["bf16", "f32", "f16"], 1)]
+         ([2_500_001, 6208], ["f32"], 0), ([6_100_003, 6208], ["f32"], 0), (MANY[:100], ["bf16", "f32", "f16"], 1)]
 
 
 @pytest.mark.parametrize("sizes,kinds,shift", ADAMS, ids=lambda a: str(len(a)) if isinstance(a, list) else str(a))
