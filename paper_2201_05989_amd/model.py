@@ -45,7 +45,7 @@ class HashGridModel:
         self.weights_half = self.weights.half()
         self._net_m, self._net_v = torch.zeros_like(self.weights), torch.zeros_like(self.weights)
         self._W, self._n_weights = self._views(self.weights_half), self.weights.numel()
-        self.steps = 0
+        self._steps, self.grad_stats = 0, None
         self._loss_sum = torch.zeros(1, dtype=torch.float64, device="cuda")
         self._scratch = torch.empty(HG_TRAIN_SCRATCH_BYTES, dtype=torch.uint8, device="cuda")
         self._state = hashgrid_train_state(
@@ -53,8 +53,20 @@ class HashGridModel:
             weights_adam=hashgrid_adam_config(0.0, 0.9, 0.99, 1e-15, 0.0), loss_sum=self._loss_sum.data_ptr(),
             scratch=self._scratch.data_ptr())
         self._buf_B = 0
-        self._max_grad_norm = self.grad_stats = self._grads = None
+        self._max_grad_norm = self._grads = None
         self.max_grad_norm = max_grad_norm
+
+    @property
+    def steps(self) -> int:
+        """Calls of step so far; set it to resume.  (With max_grad_norm the optimiser's own count, without the steps that were left
+        out, is grad_stats.steps on the device, and is set along with it.)"""
+        return self._steps
+
+    @steps.setter
+    def steps(self, n: int) -> None:
+        self._steps = n
+        if self.grad_stats is not None:
+            self.grad_stats.steps.fill_(n)
 
     @property
     def max_grad_norm(self) -> float | None:
@@ -70,7 +82,7 @@ class HashGridModel:
                 self.grad_stats = GradStats()
                 self._grads = torch.empty(self.tables.numel() + self._n_weights, device="cuda")
             if self._max_grad_norm is None:  # the device counts on from the steps that were taken without it
-                self.grad_stats.steps.fill_(self.steps)
+                self.grad_stats.steps.fill_(self._steps)
         self._max_grad_norm = bound
 
     def _views(self, flat):
@@ -131,8 +143,8 @@ class HashGridModel:
         B = x.shape[0]
         self._buffers(B)
         clip = None if self._max_grad_norm is None else (self._max_grad_norm, self.grad_stats, self._grads)
-        self.grid.train_step(self._train_state(B), x, target, self._y, self._dy, self.steps + 1, clip=clip)
-        self.steps += 1
+        self.grid.train_step(self._train_state(B), x, target, self._y, self._dy, self._steps + 1, clip=clip)
+        self._steps += 1
         self._n_last = B * self.n_out
 
     def last_loss(self) -> float:

@@ -177,6 +177,9 @@ def test_the_bound_may_be_changed_between_steps():
     m.max_grad_norm = 1.0
     m.step(x, target)
     assert int(m.grad_stats.steps) == 7 == m.steps
+    m.steps = 100              # resumed from elsewhere
+    m.step(x, target)
+    assert int(m.grad_stats.steps) == 101 == m.steps
 
 
 def test_status_codes_and_an_empty_batch():
