@@ -3,11 +3,11 @@
 //
 // Memory bound, as the step on one array is (adam.hip): a scalar with a gradient costs 12 bytes of reads and 12 to 14 of writes
 // beside its gradient; the clipped gradient is never stored.  Scalars without a gradient keep every bit, but memory is read and
-// written by the line: where one of the 32 scalars that share a line of each fp32 array has a gradient, all of the line is
-// read and written back, past the caches where they do not hold it all from one step to the next.  Left out lane by lane, the stores leave lines with holes behind, which
-// cost the memory more than whole ones (norm and step, fp32 gradients: 58 M scalars of which 22 % have one 437 -> 321 us, 408 M
-// with 63 % 2.92 -> 2.61 ms, 12 M with 95 % 85 -> 75; lines passed by the caches and left out lane by lane 466, 3.80, 76).
-// Lines in which no scalar has a gradient cost their gradient's bytes.
+// written by the line: where one of the 32 scalars that share a line of each fp32 array has a gradient, all of the line is read
+// and written back, past the caches where they do not hold it all from one step to the next.  Left out lane by lane, the
+// stores leave lines with holes behind, which cost the memory more than whole ones (norm and step, fp32 gradients: 58 M scalars
+// of which 22 % have one 437 -> 321 us, 408 M with 63 % 2.92 -> 2.61 ms, 12 M with 95 % 85 -> 75; lines passed by the caches and left
+// out lane by lane 466, 3.80, 76).  Lines in which no scalar has a gradient cost their gradient's bytes.
 // (Step alone: 408 M scalars 2.3 ms, 12.2 GB in whole lines at 5.3 TB/s, where a large copy reaches 4.9; 12 M 62 us.)
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -237,9 +237,9 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
     if (hg::misaligned(t.params_master, 4) || hg::misaligned(t.m, 4) || hg::misaligned(t.v, 4) ||
         hg::misaligned(t.grad, hg::dtype_bytes(t.grad_dtype)) || (t.params_half && hg::misaligned(t.params_half, 2)))
       return HG_ERR_INVALID_ARG;
-    auto add = [&](const void* p, uint32_t bytes, bool written) {
+    auto add = [&](const void* p, uint32_t each, bool written) {
       const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-      ranges[n_ranges++] = hg::Range{at, at + t.n_scalars * bytes, written};
+      ranges[n_ranges++] = hg::Range{at, at + t.n_scalars * each, written};
     };
     add(t.params_master, 4, true);
     add(t.m, 4, true);
@@ -253,9 +253,8 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
   if (n_ranges == 0 && !stats) return HG_OK;
   if (hg::ranges_clash(ranges, n_ranges)) return HG_ERR_INVALID_ARG;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const hg::Reach reach = bytes > hg::kCacheBytes                           ? hg::Reach::kAll
-                          : bytes + 14 * scalars > hg::kResidentBytes ? hg::Reach::kState
-                                                                      : hg::Reach::kNone;
+  const uint64_t all = bytes + 14 * scalars;  // with value, moments and copy
+  const hg::Reach reach = bytes > hg::kCacheBytes ? hg::Reach::kAll : all > hg::kResidentBytes ? hg::Reach::kState : hg::Reach::kNone;
   // Half as many workgroups where that still leaves each some ten units: with fewer streams open the memory is faster (norm and
   // step on 58 M scalars 305 us with 512 and 320 with 1024, on 12 M 74.3 and 73.5, on 7 M 48.7 and 46.5).
   const uint32_t most = scalars > (32u << 20) ? hg::kMaxListGroups / 2 : hg::kMaxListGroups;

@@ -107,8 +107,8 @@ inline uint32_t unit_for(uint64_t scalars) {
 inline uint32_t step_unit_for(uint64_t scalars) { return scalars > (8u << 20) ? kLargeUnit : kSmallUnit; }
 
 // Whether a list's gradients are too many for the last-level cache to hold from the norm's reading to the next: both then
-// pass by the caches.  (Measured on either side: norm and optimiser step on 408 M fp32 gradients, 1.6 GB, 2525 us passing by and
-// 2608 through the caches, on 58 M, 232 MB, 353 and 320, on 12 M 81 and 75.)
+// pass by the caches.  (Measured on either side: norm and optimiser step on 408 M fp32 gradients, 1.6 GB, 2.57 ms passing by and
+// 2.61 through the caches, the norm of as many fp16 ones 130 us and 145; on 58 M fp32, 232 MB, 353 and 320, on 12 M 81 and 75.)
 constexpr uint64_t kCacheBytes = 256u << 20;
 
 inline uint32_t groups_of(uint32_t units, uint32_t most = kMaxListGroups) { return units < most ? (units ? units : 1) : most; }
