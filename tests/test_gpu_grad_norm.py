@@ -251,6 +251,49 @@ def test_one_tensor_and_a_step_of_the_hosts_is_adam_step_bit_for_bit(n, kind, l2
         assert all(torch.equal(s, t) for s, t in zip(a, b))
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("touched", [1.0, 0.05])
+def test_what_lies_around_the_arrays_and_what_has_no_gradient_keeps_every_bit(kind, touched):
+    """Odd stretches within larger arrays, each a different way off 16 bytes; lines are written back whole, so scalars without
+    a gradient beside some that have one are written too, with what was there (NaN moments among it)."""
+    n = 30_011
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    big = [torch.randn(n + 20, device="cuda", generator=gen) for _ in range(3)]
+    big[2].abs_()
+    half = big[0].half() if kind != "bf16" else big[0].bfloat16()
+    grad = (torch.randn(n + 20, device="cuda", generator=gen) * (torch.rand(n + 20, device="cuda", generator=gen) < touched)).to(TYPES[kind])
+    arrays = [*big, half, grad]
+    at = [slice(k, k + n) for k in (1, 2, 3, 5, 7)]
+    p, m, v, h, g = (a[s] for a, s in zip(arrays, at))
+    h.copy_(p)
+    quiet = g == 0
+    m[quiet] = float("nan")
+    v[quiet] = -1.0
+    before = [a.clone() for a in arrays]
+    adam_steps([AdamTensor(p, g, m, v, h)], step=3, zero_grad=False)
+    for a, was, s in zip(arrays, before, at):
+        inside = torch.zeros(a.numel(), dtype=torch.bool, device="cuda")
+        inside[s] = ~quiet
+        words = torch.int32 if a.dtype == torch.float32 else torch.int16
+        assert torch.equal(a.view(words)[~inside], was.view(words)[~inside])
+        assert a is grad or not torch.equal(a[inside], was[inside])
+    assert torch.equal(grad, before[4])
+
+
+def test_two_calls_at_once_with_stats_of_their_own():
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    grads = [[torch.randn(n, device="cuda").to(t) for n in (6_000_011, 70_001)] for t in (torch.float32, torch.float16)]
+    stats, outs = [GradStats() for _ in range(2)], [[torch.empty_like(g) for g in gs] for gs in grads]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, gs, st, o in zip(streams, grads, stats, outs):
+            clip_grads(gs, 1.0, st, out=o, stream=s)
+    torch.cuda.synchronize()
+    for gs, st, o in zip(grads, stats, outs):
+        check_norm(gs, st, 1.0)
+        assert all(torch.equal(b, (a.float() * st.factor).to(a.dtype)) for a, b in zip(gs, o))
+
+
 def test_several_lists_after_one_norm_make_one_step():
     items = tensors_for_adam([500, 300, 7], ["f32"], 9, 0, 0.0)
     stats = GradStats()
@@ -329,6 +372,24 @@ def test_another_stream_and_a_captured_step():
             for x, y in zip((s.params_master, s.m, s.v, s.grad), (t.params_master, t.m, t.v, t.grad)):
                 assert torch.equal(x, y)
         assert all(torch.equal(x, y) for x, y in zip(*outs))
+
+
+def test_two_captured_calls_that_share_stats_one_after_the_other():
+    lists = [[torch.zeros(n, device="cuda") for n in sizes] for sizes in ([2_200_003, 17], [900, 31_007, 5])]
+    stats, graphs, stream = GradStats(), [], torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    for grads in lists:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            clip_grads(grads, 0.5, stats)
+    for i in range(3):
+        for grads, graph in zip(lists, graphs):
+            for g in grads:
+                g.normal_()
+            before = [g.clone() for g in grads]
+            graph.replay()
+            check_norm(before, stats, 0.5)
+            assert all(torch.equal(g, b * stats.factor) for g, b in zip(grads, before))
 
 
 def test_a_stream_given_as_an_argument():

@@ -3,9 +3,11 @@ would be launched, so no device is needed."""
 import ctypes
 import math
 
+import numpy as np
 import pytest
 import torch
 
+from oracle import grad_norm_oracle as gno
 from paper_2201_05989_amd import AdamList, AdamTensor, GradList, HashGridError, binding
 
 A = 1 << 20  # an address that nothing reads
@@ -22,6 +24,19 @@ def adam(*rows, **kw):
         d.update(row)
         return binding.hashgrid_adam_tensor(**d)
     return (binding.hashgrid_adam_tensor * len(rows))(*[one(i, r) for i, r in enumerate(rows)])
+
+
+def test_the_oracle_s_norm_and_factor():
+    three, four = np.array([[3.0]], dtype=np.float32), np.array([0.0, 4.0], dtype=np.float16)
+    assert gno.norm([three, four]) == 5 and gno.norm([three, four], 0.5) == 2.5 and gno.norm([]) == 0
+    assert gno.factor(gno.norm([three, four]), 1.0) == np.longdouble(1) / 5 and gno.factor(5.0, 5.0) == 1 and gno.factor(5.0, 0.0) == 0
+    # squares beyond the range of 64 bits' neighbours, none lost: 1e-44 is a subnormal fp32
+    huge, tiny = np.full(4, 3e38, dtype=np.float32), np.full(9, 1e-44, dtype=np.float32)
+    assert abs(gno.norm([huge]) / (2 * np.longdouble(huge[0])) - 1) < 1e-18
+    assert abs(gno.norm([tiny]) / (3 * np.longdouble(tiny[0])) - 1) < 1e-18
+    for bad in (np.inf, -np.inf, np.nan):
+        n = gno.norm([three, np.array([bad], dtype=np.float32)])
+        assert not np.isfinite(n) and gno.factor(n, 1.0) == 0
 
 
 def test_the_structures_are_the_header_s():
