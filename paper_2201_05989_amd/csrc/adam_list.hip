@@ -268,7 +268,9 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
       if (t.n_scalars == 0) continue;
       list.item[list.n_items++] =
           hg::AdamItem{hg::AdamState{t.params_master, static_cast<_Float16*>(t.params_half), t.m, t.v}, t.grad,
-                       hg::next_place(list, t.n_scalars, t.grad_dtype, t.half_dtype & 15), hg::adam_args(t.cfg, step ? step : 1u)};
+                       hg::next_place(list, t.n_scalars, t.grad_dtype, t.half_dtype & 15),
+                       step ? hg::adam_args(t.cfg, step)
+                            : hg::AdamArgs{t.cfg.lr, t.cfg.beta1, t.cfg.beta2, t.cfg.eps, t.cfg.l2_reg, 0.0f, 0.0f}};
     }
     if (list.n_items == 0 && n_ranges) break;
     const uint32_t groups = hg::groups_of(list.units, most);
