@@ -433,8 +433,8 @@ typedef struct {
 hg_status hashgrid_grad_norm(uint32_t n_tensors, const hashgrid_grad* grads, float grad_scale, float max_norm,
                              hashgrid_grad_stats* stats, void* stream);
 
-/* hashgrid_grad_norm, and then out_i = factor * grads_i, each product rounded once to the tensor's type: the gradients keep their
- * loss scale.  factor == 0 (max_norm 0, or a gradient that is not finite) writes zeros, which hashgrid_adam_step passes over.
+/* hashgrid_grad_norm, and then out_i = factor * grads_i, each product rounded (nearest even) to the tensor's type from fp32 or,
+ * fp16 ones, at once: the gradients keep their loss scale.  factor == 0 (max_norm 0, or a gradient that is not finite) writes zeros, which hashgrid_adam_step passes over.
  * (hashgrid_adam_steps clips on its way and needs the norm alone.)
  *   out  [n_tensors]  HOST array of device pointers to arrays of the gradients' types and sizes; out[i] == grads[i].data
  *                     is in place.  NULL: all in place; where factor is 1 nothing is written then.

@@ -3,7 +3,11 @@ precision) and the fp64 optimiser oracle, on lists of tensors of several types, 
 
 Bars.  norm: squares and sums in 64 bits (a chain of at most 10^5 additions: 10^5 2^-53 < 2^-36 relative), rounded once to fp32:
 2^-24 relative, here 2^-24 (1 + 2^-10), and half the smallest subnormal.  factor: one 64-bit quotient rounded once: the same.  Clipped
-gradients: one fp32 product with the factor on the device, rounded once to the type: bit for bit what torch gives.  The
+gradients: fp32 ones are the fp32 product with the factor on the device, bit for bit.  16-bit ones are that product rounded to the type, or
+the exact product rounded at once (one instruction of this machine does that for fp16): g (11 bits) times the factor (24 bits) is exact in
+64 bits, P; rounded to fp32 and then to the type it is off by at most 2^-24 |P| and then half a step of a value of at most
+(1 + 2^-24) |P|, eps / 2 of it; half the smallest subnormal of either type where P is that small.  (An fp32 product that lies half-way between
+two fp16 values by its own rounding goes to the even one, the exact one to the nearer: 1120.5000155 steps to 1120 and 1121.)  The
 optimiser step: bit for bit hashgrid_adam_step's where both get the same gradient and the same step number from the host; against
 the oracle the bars of test_gpu_adam.py, with the gradient's own two roundings (scale, product: 2^-23 relative) on top.
 """
@@ -23,6 +27,19 @@ HALF_ULP = 2.0 ** -24 * (1 + 2.0 ** -10)
 
 def cpu64(t):
     return t.detach().cpu().double().numpy()
+
+
+def clipped_right(out, g, factor):
+    """out = factor * g, as far as the type's rounding goes (see above); exact zeros for a factor of 0."""
+    assert out.dtype == g.dtype
+    if float(factor) == 0:
+        return bool((out == 0).all())
+    if g.dtype == torch.float32:
+        return torch.equal(out, g * factor)
+    info = torch.finfo(g.dtype)
+    exact = g.double() * factor.double()
+    bar = (info.eps / 2 * (1 + 2.0 ** -24) + 2.0 ** -24) * exact.abs() + info.smallest_normal * info.eps / 2 * (1 + 2.0 ** -20)
+    return bool(((out.double() - exact).abs() <= bar).all())
 
 
 def make(sizes, dtype, seed, shift=0, scale=1.0, guard=None):
@@ -102,7 +119,7 @@ def test_no_gradient_is_too_large_or_too_small(value, kind):
     out = torch.empty_like(g)
     clip_grads([g], bound, stats, out=[out])
     # subnormals as anywhere: rounded, not flushed
-    assert torch.equal(out, torch.zeros_like(g) if float(stats.factor) == 0 else (g.float() * stats.factor).to(g.dtype))
+    assert clipped_right(out, g, stats.factor)
 
 
 CLIPS = [MANY, [1], [0, 3], [2049, 1, 7], [7, 4096, 1, 1, 300, 65537], [9] * 200, [3_000_001, 65]]
@@ -122,15 +139,16 @@ def test_clipping_in_place_and_into_other_arrays(kind, sizes):
             clip_grads(grads, bound, stats, out=outs)
             check_norm(grads, stats, bound)
             for g, o in zip(grads, outs):
-                assert torch.equal(o, (g.float() * stats.factor).to(g.dtype))
+                assert clipped_right(o, g, stats.factor)
             assert torch.equal(flat, before) and bool((big[rest] == 7.0).all())
         clip_grads(grads, 1e9, stats)          # nothing to clip
         assert torch.equal(flat, before)
         norm = clip_grads(grads, 0.01, stats)  # in place
         assert norm is stats.norm
-        want = before.clone()
-        want[shift:shift + sum(sizes)] = (before[shift:shift + sum(sizes)].float() * stats.factor).to(before.dtype)
-        assert torch.equal(flat, want)         # what lies around the tensors too
+        inside = slice(shift, shift + sum(sizes))
+        assert clipped_right(flat[inside], before[inside], stats.factor)
+        before[inside] = flat[inside]
+        assert torch.equal(flat, before)       # what lies around the tensors too
 
 
 @pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
@@ -280,6 +298,21 @@ def test_what_lies_around_the_arrays_and_what_has_no_gradient_keeps_every_bit(ki
     assert torch.equal(grad, before[4])
 
 
+def test_products_next_to_the_middle_between_two_values():
+    # the fp32 product of these is a tie between two fp16 (bf16) values that the exact product is not
+    g = torch.tensor([-0.65869140625, 2.130859375, 0.8071289062], dtype=torch.float64)
+    for kind in ("f16", "bf16"):
+        a = torch.randn(400_000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).to(TYPES[kind])
+        a[:3] = g.to(TYPES[kind]).cuda()
+        stats, out = GradStats(), torch.empty_like(a)
+        for bound in (0.1, 0.256789, 0.31):
+            clip_grads([a], bound, stats, out=[out])
+            assert clipped_right(out, a, stats.factor)
+            back = torch.empty_like(a)
+            clip_grads([a[k:k + 4000] for k in range(0, 400_000, 4000)], bound, stats, out=[back[k:k + 4000] for k in range(0, 400_000, 4000)])
+            assert torch.equal(out, back)  # however the scalars are dealt out
+
+
 def test_two_calls_at_once_with_stats_of_their_own():
     streams = [torch.cuda.Stream() for _ in range(2)]
     grads = [[torch.randn(n, device="cuda").to(t) for n in (6_000_011, 70_001)] for t in (torch.float32, torch.float16)]
@@ -291,7 +324,7 @@ def test_two_calls_at_once_with_stats_of_their_own():
     torch.cuda.synchronize()
     for gs, st, o in zip(grads, stats, outs):
         check_norm(gs, st, 1.0)
-        assert all(torch.equal(b, (a.float() * st.factor).to(a.dtype)) for a, b in zip(gs, o))
+        assert all(clipped_right(b, a, st.factor) for a, b in zip(gs, o))
 
 
 def test_several_lists_after_one_norm_make_one_step():
@@ -412,7 +445,7 @@ def test_arrays_beyond_32_bits():
     stats = GradStats()
     clip_grads([g], 15.7, stats)   # 3, 4, 12, 84, 132: norm 157
     assert float(stats.norm) == 157.0 and abs(float(stats.factor) - 0.1) <= 1e-8
-    assert torch.equal(g[where], (torch.tensor([3.0, 4.0, 12.0, 84.0, 132.0], device="cuda") * stats.factor).half())
+    assert clipped_right(g[where], torch.tensor([3.0, 4.0, 12.0, 84.0, 132.0], device="cuda").half(), stats.factor)
     assert int(torch.count_nonzero(g)) == 5
     del g
     n = (1 << 30) + 1031
