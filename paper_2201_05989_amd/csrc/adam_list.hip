@@ -225,8 +225,6 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
   if (n_tensors > HG_MAX_TENSORS) return HG_ERR_UNSUPPORTED;
   if ((n_tensors && !tensors) || (step == 0) == (stats == nullptr)) return HG_ERR_INVALID_ARG;
   if (!(grad_scale > 0.0f && grad_scale < INFINITY) || (reinterpret_cast<uintptr_t>(stats) & 15)) return HG_ERR_INVALID_ARG;
-  hg::Range ranges[5 * HG_MAX_TENSORS];
-  uint32_t n_ranges = 0;
   uint64_t scalars = 0, bytes = 0;  // (of the gradients)
   for (uint32_t i = 0; i < n_tensors; ++i) {
     const hashgrid_adam_tensor& t = tensors[i];
@@ -237,21 +235,19 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
     if (hg::misaligned(t.params_master, 4) || hg::misaligned(t.m, 4) || hg::misaligned(t.v, 4) ||
         hg::misaligned(t.grad, hg::dtype_bytes(t.grad_dtype)) || (t.params_half && hg::misaligned(t.params_half, 2)))
       return HG_ERR_INVALID_ARG;
-    auto add = [&](const void* p, uint32_t each, bool written) {
-      const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-      ranges[n_ranges++] = hg::Range{at, at + t.n_scalars * each, written};
-    };
-    add(t.params_master, 4, true);
-    add(t.m, 4, true);
-    add(t.v, 4, true);
-    add(t.grad, hg::dtype_bytes(t.grad_dtype), zero_grad != 0);
-    if (t.params_half) add(t.params_half, 2, true);
     scalars += t.n_scalars;
     bytes += t.n_scalars * hg::dtype_bytes(t.grad_dtype);
   }
   if (scalars > HG_MAX_TENSOR_SCALARS) return HG_ERR_UNSUPPORTED;
-  if (n_ranges == 0 && !stats) return HG_OK;
-  if (hg::ranges_clash(ranges, n_ranges)) return HG_ERR_INVALID_ARG;
+  if (scalars == 0 && !stats) return HG_OK;
+  const bool clash = hg::ranges_clash<5>(n_tensors, [&](int kind, uint32_t i) {
+    const hashgrid_adam_tensor& t = tensors[i];
+    const void* const array = kind == 0 ? t.params_master : kind == 1 ? t.m : kind == 2 ? t.v : kind == 3 ? t.grad : t.params_half;
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(array);
+    const uint64_t each = kind < 3 ? 4 : kind == 3 ? hg::dtype_bytes(t.grad_dtype) : t.params_half ? 2 : 0;
+    return hg::Range{begin, begin + t.n_scalars * each, kind != 3 || zero_grad};
+  });
+  if (clash) return HG_ERR_INVALID_ARG;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const uint64_t all = bytes + 14 * scalars;  // with value, moments and copy
   const hg::Reach reach = bytes > hg::kCacheBytes ? hg::Reach::kAll : all > hg::kResidentBytes ? hg::Reach::kState : hg::Reach::kNone;
@@ -272,7 +268,7 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
                        step ? hg::adam_args(t.cfg, step)
                             : hg::AdamArgs{t.cfg.lr, t.cfg.beta1, t.cfg.beta2, t.cfg.eps, t.cfg.l2_reg, 0.0f, 0.0f}};
     }
-    if (list.n_items == 0 && n_ranges) break;
+    if (list.n_items == 0 && scalars) break;
     const uint32_t groups = hg::groups_of(list.units, most);
     const auto kernel = hg::kernels[zero_grad ? 1 : 0][(int)reach];
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(hg::kListThreads), 0, s, list, grad_scale, stats);

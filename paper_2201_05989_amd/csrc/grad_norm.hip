@@ -14,24 +14,12 @@
 // and 32, 7.3 TB/s, the second reading from the last-level cache), and nothing where the factor is 1 and it is in place.
 #include <hip/hip_runtime.h>
 #include <math.h>
-#include <algorithm>
 #include <stdint.h>
 
 #include "hashgrid.h"
 #include "tensor_list.hpp"
 
 namespace hg {
-
-bool ranges_clash(Range* r, const uint32_t n) {
-  std::sort(r, r + n, [](const Range& a, const Range& b) { return a.begin < b.begin; });
-  uintptr_t any = 0, written = 0;  // ends of the ranges before this one
-  for (uint32_t i = 0; i < n; ++i) {
-    if (r[i].begin < (r[i].written ? any : written)) return true;
-    any = std::max(any, r[i].end);
-    if (r[i].written) written = std::max(written, r[i].end);
-  }
-  return false;
-}
 
 namespace {
 
@@ -317,16 +305,14 @@ extern "C" hg_status hashgrid_clip_grads(uint32_t n_tensors, const hashgrid_grad
   uint64_t scalars, bytes;
   const hg_status ok = hg::check_grads(n_tensors, grads, grad_scale, max_norm, stats, &scalars, &bytes);
   if (ok != HG_OK) return ok;
-  hg::Range ranges[2 * HG_MAX_TENSORS];
-  uint32_t n_ranges = 0;
-  for (uint32_t i = 0; i < n_tensors; ++i) {
-    if (grads[i].n_scalars == 0) continue;
-    if (out && hg::bad_array(out[i], grads[i].dtype)) return HG_ERR_INVALID_ARG;
+  for (uint32_t i = 0; out && i < n_tensors; ++i)
+    if (grads[i].n_scalars && hg::bad_array(out[i], grads[i].dtype)) return HG_ERR_INVALID_ARG;
+  const bool clash = hg::ranges_clash<2>(n_tensors, [&](int kind, uint32_t i) {
     const uintptr_t size = grads[i].n_scalars * hg::dtype_bytes(grads[i].dtype);
     const uintptr_t from = reinterpret_cast<uintptr_t>(grads[i].data), to = out ? reinterpret_cast<uintptr_t>(out[i]) : from;
-    ranges[n_ranges++] = hg::Range{to, to + size, true};
-    if (to != from) ranges[n_ranges++] = hg::Range{from, from + size, false};
-  }
-  if (hg::ranges_clash(ranges, n_ranges)) return HG_ERR_INVALID_ARG;
+    if (kind == 0) return hg::Range{to, to + size, true};
+    return to == from ? hg::Range{} : hg::Range{from, from + size, false};
+  });
+  if (clash) return HG_ERR_INVALID_ARG;
   return hg::launch(n_tensors, grads, true, out, scalars, bytes, grad_scale, max_norm, stats, static_cast<hipStream_t>(stream));
 }
