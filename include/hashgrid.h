@@ -40,7 +40,8 @@
  *     no synchronisation), so calls can be recorded into a HIP graph.  What a call derives on the
  *     host from its scalar arguments travels as kernel arguments and is fixed at capture: a
  *     replayed hashgrid_adam_step repeats the bias correction of the `step` it was recorded with
- *     (callers that replay update the node's arguments or record one node per step).
+ *     (callers that replay update the node's arguments or record one node per step;
+ *     hashgrid_adam_steps and hashgrid_train_step_clipped can count the steps on the device instead).
  */
 #ifndef HASHGRID_H
 #define HASHGRID_H
