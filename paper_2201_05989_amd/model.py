@@ -45,7 +45,9 @@ class HashGridModel:
         self.weights_half = self.weights.half()
         self._net_m, self._net_v = torch.zeros_like(self.weights), torch.zeros_like(self.weights)
         self._W, self._n_weights = self._views(self.weights_half), self.weights.numel()
-        self._steps, self.grad_stats = 0, None
+        # calls of step; the optimiser's steps as the host knows them, without a bound; how many of those grad_stats.steps holds
+        self._steps = self._taken = self._counted = 0
+        self.grad_stats = None
         self._loss_sum = torch.zeros(1, dtype=torch.float64, device="cuda")
         self._scratch = torch.empty(HG_TRAIN_SCRATCH_BYTES, dtype=torch.uint8, device="cuda")
         self._state = hashgrid_train_state(
@@ -59,14 +61,15 @@ class HashGridModel:
     @property
     def steps(self) -> int:
         """Calls of step so far; set it to resume.  (With max_grad_norm the optimiser's own count, without the steps that were left
-        out, is grad_stats.steps on the device, and is set along with it.)"""
+        out and with the replays of a captured one, is grad_stats.steps on the device, and is set along with it.)"""
         return self._steps
 
     @steps.setter
     def steps(self, n: int) -> None:
-        self._steps = n
+        self._steps = self._taken = n
         if self.grad_stats is not None:
             self.grad_stats.steps.fill_(n)
+            self._counted = n
 
     @property
     def max_grad_norm(self) -> float | None:
@@ -74,15 +77,20 @@ class HashGridModel:
 
     @max_grad_norm.setter
     def max_grad_norm(self, bound: float | None) -> None:
-        """May be changed between steps (outside a captured one: the bound is part of the capture)."""
+        """May be changed between steps (outside a captured one: the bound is part of the capture).  Without a bound the host
+        counts the optimiser's steps, with one the device does: each goes on from the other's count, for which taking the bound off
+        waits for torch's current stream."""
         if bound is not None:
             if not bound >= 0:
                 raise HashGridError(f"max_grad_norm must be None or at least 0, not {bound!r}")
             if self.grad_stats is None:
                 self.grad_stats = GradStats()
                 self._grads = torch.empty(self.tables.numel() + self._n_weights, device="cuda")
-            if self._max_grad_norm is None:  # the device counts on from the steps that were taken without it
-                self.grad_stats.steps.fill_(self._steps)
+            if self._max_grad_norm is None and self._taken != self._counted:  # the steps taken since the device's count was read
+                self.grad_stats.steps.add_(self._taken - self._counted)
+                self._counted = self._taken
+        elif self._max_grad_norm is not None:
+            self._taken = self._counted = int(self.grad_stats.steps)
         self._max_grad_norm = bound
 
     def _views(self, flat):
@@ -143,8 +151,10 @@ class HashGridModel:
         B = x.shape[0]
         self._buffers(B)
         clip = None if self._max_grad_norm is None else (self._max_grad_norm, self.grad_stats, self._grads)
-        self.grid.train_step(self._train_state(B), x, target, self._y, self._dy, self._steps + 1, clip=clip)
+        self.grid.train_step(self._train_state(B), x, target, self._y, self._dy, self._taken + 1, clip=clip)
         self._steps += 1
+        if clip is None:
+            self._taken += 1
         self._n_last = B * self.n_out
 
     def last_loss(self) -> float:
