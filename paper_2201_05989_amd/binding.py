@@ -8,6 +8,7 @@ entry points raises.
 from __future__ import annotations
 
 import ctypes
+import itertools
 import math
 import os
 from dataclasses import dataclass
@@ -572,6 +573,9 @@ def clip_grads(grads, max_norm: float, stats: GradStats, out=None, grad_scale: f
     return stats.norm
 
 
+_stamps = itertools.count(1)
+
+
 @dataclass(eq=False)
 class AdamTensor:
     """One tensor of adam_steps: fp32 master copy and moments, gradient (fp32, fp16 or bf16), 16-bit working copy or None, and
@@ -587,14 +591,19 @@ class AdamTensor:
     eps: float = 1e-15
     l2_reg: float = 0.0
 
+    # What an AdamList goes by: a number that no other AdamTensor has had, nor this one before it was last changed.
     def __setattr__(self, name, value):
         self.__dict__[name] = value
-        self.__dict__["_changes"] = self.__dict__.get("_changes", 0) + 1  # (what an AdamList goes by)
+        self.__dict__["_stamp"] = next(_stamps)
+
+    def __setstate__(self, state):  # of a copy
+        self.__dict__.update(state)
+        self.__dict__["_stamp"] = next(_stamps)
 
 
 class AdamList:
-    """The tensors of a model that one optimiser step updates, looked over once for many calls; a tensor that was replaced, whose
-    memory has moved or whose hyper-parameters have changed is looked up again.  grads: their GradList."""
+    """The tensors of a model that one optimiser step updates, looked over once for many calls; a tensor that was replaced (in
+    `tensors` or in its AdamTensor), whose memory has moved or whose hyper-parameters have changed is looked up again.  grads: their GradList."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -620,17 +629,17 @@ class AdamList:
         self._flat, self._array = flat, (hashgrid_adam_tensor * len(rows))(*rows)
         self._grads = GradList([t.grad for t in self.tensors])
         self._at = list(map(_data_ptr, flat))
-        self._changes = [t._changes for t in self.tensors]
+        self._seen = [t._stamp for t in self.tensors]
 
     def _current(self):
-        if [t._changes for t in self.tensors] != self._changes or list(map(_data_ptr, self._flat)) != self._at:
+        if [t._stamp for t in self.tensors] != self._seen or list(map(_data_ptr, self._flat)) != self._at:
             self._look_up()
         _on_current_device(self._device, "tensors")
         return self
 
     @property
     def grads(self) -> GradList:
-        if [t._changes for t in self.tensors] != self._changes:
+        if [t._stamp for t in self.tensors] != self._seen:
             self._look_up()
         return self._grads
 

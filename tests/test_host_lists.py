@@ -1,0 +1,84 @@
+"""Lists of tensors (AdamList and its GradList) that change between two calls, on the CPU: host tensors that pass for the current device's, so
+that what a list tells the library can be read from its descriptions.  Nothing is launched here."""
+import copy
+
+import pytest
+import torch
+
+from paper_2201_05989_amd import AdamList, AdamTensor, binding
+
+
+class OnDevice(torch.Tensor):
+    is_cuda = True
+
+    def get_device(self):
+        return 0
+
+    def __deepcopy__(self, memo):
+        return self.as_subclass(torch.Tensor).clone().as_subclass(OnDevice)
+
+
+@pytest.fixture(autouse=True)
+def current_device(monkeypatch):
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+
+
+def tensor(n, dtype=torch.float32):
+    return torch.zeros(n, dtype=dtype).as_subclass(OnDevice)
+
+
+def item(n, **kw):
+    return AdamTensor(tensor(n), tensor(n), tensor(n), tensor(n), tensor(n, torch.float16), **kw)
+
+
+def told(model):
+    """What the library is told of each tensor."""
+    a = model._current()
+    assert len(a) == len(a._array)
+    return [(r.params_master, r.params_half, r.grad, r.m, r.v, r.n_scalars, r.cfg.lr) for r in a._array]
+
+
+def wanted(items):
+    return [(t.params_master.data_ptr(), t.params_half.data_ptr(), t.grad.data_ptr(), t.m.data_ptr(), t.v.data_ptr(),
+             t.params_master.numel(), torch.tensor(t.lr).item()) for t in items]
+
+
+def grads_told(grads):
+    return [(g.data, g.n_scalars, g.dtype) for g in grads._current()._array]
+
+
+def test_a_tensor_that_is_replaced_in_the_list_is_looked_up_again():
+    model = AdamList([item(8), item(5)])
+    first = told(model)
+    assert first == wanted(model.tensors)
+    model.tensors[0] = item(8)
+    assert told(model) == wanted(model.tensors) != first
+    assert [g[0] for g in grads_told(model.grads)] == [t.grad.data_ptr() for t in model.tensors]
+    model.tensors[1] = item(12)      # of another size
+    assert [g[:2] for g in grads_told(model.grads)] == [(t.grad.data_ptr(), t.grad.numel()) for t in model.tensors]
+    assert told(model) == wanted(model.tensors)
+
+
+def test_tensors_that_change_places_keep_their_own_hyper_parameters():
+    model = AdamList([item(8, lr=0.5), item(8, lr=0.25)])
+    told(model)
+    model.tensors.reverse()
+    assert told(model) == wanted(model.tensors) and [t.lr for t in model.tensors] == [0.25, 0.5]
+
+
+@pytest.mark.parametrize("how", [copy.copy, copy.deepcopy])
+def test_a_copy_is_another_tensor(how):
+    model = AdamList([item(8)])
+    told(model)
+    other = model.tensors[0] = how(model.tensors[0])
+    assert told(model) == wanted(model.tensors)
+    other.lr, other.grad = 0.125, tensor(8)
+    assert told(model) == wanted(model.tensors)
+
+
+def test_lists_that_grow_and_shrink():
+    model = AdamList([item(8)])
+    model.tensors.append(item(3))
+    assert told(model) == wanted(model.tensors)
+    del model.tensors[0]
+    assert told(model) == wanted(model.tensors) and len(model.grads) == 1
