@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import itertools
 import math
+import operator
 import os
 from dataclasses import dataclass
 
@@ -515,12 +516,19 @@ def _one_device(tensors):
     return devices.pop() if devices else None
 
 
-_data_ptr = torch.Tensor.data_ptr
+_data_ptr, _bytes = torch.Tensor.data_ptr, operator.attrgetter("nbytes")
+
+
+def _places(tensors):
+    """Where the memory of a list's tensors lies, and how much of it is theirs: what has to be the same for a kept description to
+    hold.  (A tenth of a microsecond a tensor.)"""
+    return list(map(_data_ptr, tensors)), list(map(_bytes, tensors))
 
 
 class GradList:
-    """Gradients of a model, at most 1024 tensors of any shapes, fp32, fp16 and bf16 mixed, looked over once for many calls.  The
-    tensors keep their sizes and types; one whose memory has moved since the last call is looked up again."""
+    """Gradients of a model, at most 1024 tensors of any shapes, fp32, fp16 and bf16 mixed, looked over once for many calls.
+    One whose memory has moved since the last call, or that has more or fewer bytes of it, is looked up again (so a tensor keeps its
+    type where it keeps both)."""
 
     def __init__(self, grads):
         self.tensors = list(grads)
@@ -532,13 +540,13 @@ class GradList:
                 raise HashGridError(f"tensor {i} of the list must be a contiguous fp32, fp16 or bf16 device tensor")
         self._device = _one_device(self.tensors)
         self._kinds = [(t.dtype, t.numel()) for t in self.tensors]
-        at = [t.data_ptr() for t in self.tensors]
+        self._places = _places(self.tensors)
+        at = self._places[0]
         self._pointers = (ctypes.c_void_p * len(at))(*at)
         self._array = (hashgrid_grad * len(at))(*[(p, n, _LIST_DTYPES[dtype], 0) for p, (dtype, n) in zip(at, self._kinds)])
-        self._at = at
 
     def _current(self):
-        if list(map(_data_ptr, self.tensors)) != self._at:
+        if _places(self.tensors) != self._places:
             self._look_up()
         _on_current_device(self._device, "tensors")
         return self
@@ -603,7 +611,8 @@ class AdamTensor:
 
 class AdamList:
     """The tensors of a model that one optimiser step updates, looked over once for many calls; a tensor that was replaced (in
-    `tensors` or in its AdamTensor), whose memory has moved or whose hyper-parameters have changed is looked up again.  grads: their GradList."""
+    `tensors` or in its AdamTensor), that has other memory or another size in bytes, or whose hyper-parameters have changed is
+    looked up again.  grads: their GradList."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -628,11 +637,11 @@ class AdamList:
         self._device = _one_device(flat)
         self._flat, self._array = flat, (hashgrid_adam_tensor * len(rows))(*rows)
         self._grads = GradList([t.grad for t in self.tensors])
-        self._at = list(map(_data_ptr, flat))
+        self._places = _places(flat)
         self._seen = [t._stamp for t in self.tensors]
 
     def _current(self):
-        if [t._stamp for t in self.tensors] != self._seen or list(map(_data_ptr, self._flat)) != self._at:
+        if [t._stamp for t in self.tensors] != self._seen or _places(self._flat) != self._places:
             self._look_up()
         _on_current_device(self._device, "tensors")
         return self

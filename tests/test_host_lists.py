@@ -1,11 +1,11 @@
-"""Lists of tensors (AdamList and its GradList) that change between two calls, on the CPU: host tensors that pass for the current device's, so
+"""Lists of tensors (GradList, AdamList) that change between two calls, on the CPU: host tensors that pass for the current device's, so
 that what a list tells the library can be read from its descriptions.  Nothing is launched here."""
 import copy
 
 import pytest
 import torch
 
-from paper_2201_05989_amd import AdamList, AdamTensor, binding
+from paper_2201_05989_amd import AdamList, AdamTensor, GradList, HashGridError, binding
 
 
 class OnDevice(torch.Tensor):
@@ -82,3 +82,51 @@ def test_lists_that_grow_and_shrink():
     assert told(model) == wanted(model.tensors)
     del model.tensors[0]
     assert told(model) == wanted(model.tensors) and len(model.grads) == 1
+
+
+def shrink(t, n):
+    t.resize_(n)
+
+
+def narrow(t, n):
+    t.data = t.data[:n]
+
+
+@pytest.mark.parametrize("less", [shrink, narrow])
+def test_a_gradient_that_has_shrunk_where_it_lay_is_looked_up_again(less):
+    a, b = tensor(100), tensor(30, torch.bfloat16)
+    grads, out = GradList([a, b]), GradList([tensor(100), tensor(30, torch.bfloat16)])
+    assert grads_told(grads) == [(a.data_ptr(), 100, 0), (b.data_ptr(), 30, 2)]
+    at = b.data_ptr()
+    less(b, 7)
+    assert b.data_ptr() == at and grads_told(grads) == [(a.data_ptr(), 100, 0), (at, 7, 2)]
+    with pytest.raises(HashGridError):  # an array of the gradients' old sizes
+        binding.clip_grads(grads, 1.0, None, out=out)
+    less(a, 0)
+    assert [g[1] for g in grads_told(grads)] == [0, 7]
+
+
+def test_a_gradient_of_as_many_scalars_of_a_smaller_type_is_looked_up_again():
+    a = tensor(64)
+    grads = GradList([a])
+    grads_told(grads)
+    a.data = a.data.view(torch.bfloat16)[:64]
+    assert grads_told(grads) == [(a.data_ptr(), 64, 2)]
+
+
+@pytest.mark.parametrize("less", [shrink, narrow])
+@pytest.mark.parametrize("name", ["params_master", "params_half", "grad", "m", "v"])
+def test_an_array_of_the_optimiser_that_has_shrunk_where_it_lay_is_refused_until_all_have(name, less):
+    t = item(50)
+    model = AdamList([item(4), t])
+    told(model)
+    less(getattr(t, name), 20)
+    with pytest.raises(HashGridError):
+        model._current()
+    with pytest.raises(HashGridError):  # and not taken the second time
+        model._current()
+    for other in ("params_master", "params_half", "grad", "m", "v"):
+        if other != name:
+            less(getattr(t, other), 20)
+    assert told(model) == wanted(model.tensors) and told(model)[1][5] == 20
+    assert [g[1] for g in grads_told(model.grads)] == [4, 20]
