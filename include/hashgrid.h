@@ -476,7 +476,8 @@ hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam_tensor* te
  *             weights_adam.l2_reg is added after clipping and is not part of the norm.
  *   stats     holds the norm and the number of the optimiser step, 1 with the first call on zeroed memory
  *   grads     n_entries * F scalars and as many as `weights` behind them, fp32, device, 16-byte aligned, scratch
- * B == 0 is HG_OK and changes nothing. */
+ * HG_ERR_INVALID_ARG also where an array that is written shares memory with another one of the call.  B == 0 is HG_OK and
+ * changes nothing. */
 hg_status hashgrid_train_step_clipped(const hashgrid_t* hg, const hashgrid_train_state* st, float max_norm,
                                       hashgrid_grad_stats* stats, float* grads, uint32_t B, const float* x,
                                       const float* target, void* y, void* dLdy, void* workspace, uint64_t workspace_bytes,

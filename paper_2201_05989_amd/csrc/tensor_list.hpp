@@ -11,11 +11,11 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
-#include <algorithm>
 #include <stdint.h>
 #include <type_traits>
 
 #include "hashgrid.h"
+#include "array_ranges.hpp"
 
 namespace hg {
 
@@ -162,46 +162,6 @@ __device__ __forceinline__ void with_type(const uint32_t dtype, Fn&& f) {
     f(static_cast<_Float16*>(nullptr));
   else
     f(static_cast<__bf16*>(nullptr));
-}
-
-// Bytes of one array of a call; none where begin == end.
-struct Range {
-  uintptr_t begin, end;
-  bool written;
-};
-// Whether something is written that another array of the call shares: range_of(k, i) for k < KINDS kinds of arrays (values, gradients,
-// ...) of n <= HG_MAX_TENSORS tensors.  Each kind in the order of its addresses, as the arrays mostly come, and then all kinds
-// side by side; 2 KB of stack a kind.
-template <int KINDS, typename RangeOf>
-bool ranges_clash(const uint32_t n, RangeOf&& range_of) {
-  uint16_t order[KINDS][HG_MAX_TENSORS];
-  uint32_t count[KINDS] = {}, at[KINDS] = {};
-  for (int k = 0; k < KINDS; ++k) {
-    for (uint32_t i = 0; i < n; ++i) {
-      const Range r = range_of(k, i);
-      if (r.begin != r.end) order[k][count[k]++] = (uint16_t)i;
-    }
-    auto before = [&](uint16_t a, uint16_t b) { return range_of(k, a).begin < range_of(k, b).begin; };
-    if (!std::is_sorted(order[k], order[k] + count[k], before)) std::sort(order[k], order[k] + count[k], before);
-  }
-  uintptr_t any = 0, written = 0;  // ends of the ranges before the next one
-  for (;;) {
-    int first = -1;
-    Range r{};
-    for (int k = 0; k < KINDS; ++k) {
-      if (at[k] == count[k]) continue;
-      const Range head = range_of(k, order[k][at[k]]);
-      if (first < 0 || head.begin < r.begin) {
-        first = k;
-        r = head;
-      }
-    }
-    if (first < 0) return false;
-    if (r.begin < (r.written ? any : written)) return true;
-    any = std::max(any, r.end);
-    if (r.written) written = std::max(written, r.end);
-    ++at[first];
-  }
 }
 
 }  // namespace hg

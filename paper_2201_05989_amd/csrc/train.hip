@@ -21,6 +21,7 @@
 #include "hashgrid.h"
 #include "hashgrid_internal.hpp"
 #include "adam_device.hpp"
+#include "array_ranges.hpp"
 
 namespace hg {
 namespace {
@@ -37,6 +38,25 @@ struct Clip {
   hashgrid_grad_stats* stats;
   float* grads;  // the tables' and the weights', one after the other
 };
+
+// Whether arrays of a clipped step share memory (x and target are read only).  hashgrid_adam_steps looks at its own, but by then the
+// backward pass has added to tables_zeros: what is refused is to be refused before anything is launched.
+bool arrays_clash(const hashgrid* hg, const hashgrid_train_state& st, const Clip& clip, uint64_t n_net, uint32_t B, const float* x,
+                  const float* target, const void* y, const void* dLdy, const void* workspace, uint64_t workspace_bytes) {
+  const uint64_t n_tab = hg->total * hg->cfg.F, n_y = (uint64_t)B * hg->cfg.L * hg->cfg.F;
+  const struct {
+    const void* at;
+    uint64_t bytes;
+  } array[] = {{x, 4ull * B * hg->cfg.d}, {target, 4ull * B * st.n_out}, {y, 2 * n_y}, {dLdy, 2 * n_y}, {workspace, workspace_bytes},
+               {clip.stats, sizeof(hashgrid_grad_stats)}, {clip.grads, 4 * (n_tab + n_net)}, {st.tables, 4 * n_tab},
+               {st.tables_half, 2 * n_tab}, {st.tables_m, 4 * n_tab}, {st.tables_v, 4 * n_tab}, {st.tables_zeros, 4 * n_tab},
+               {st.weights, 4 * n_net}, {st.weights_half, 2 * n_net}, {st.weights_m, 4 * n_net}, {st.weights_v, 4 * n_net},
+               {st.loss_sum, sizeof(double)}, {st.scratch, HG_TRAIN_SCRATCH_BYTES}};
+  return ranges_clash<1>(sizeof(array) / sizeof(array[0]), [&](int, uint32_t i) {
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(array[i].at);
+    return Range{begin, begin + array[i].bytes, i >= 2};
+  });
+}
 
 // One iteration, with the optimiser step `step`; clip: with the gradients clipped, and the step that the device counts.
 hg_status train_step(const hashgrid* hg, const hashgrid_train_state* st, uint32_t B, const float* x, const float* target, void* y,
@@ -69,6 +89,9 @@ hg_status train_step(const hashgrid* hg, const hashgrid_train_state* st, uint32_
   const uint64_t need = hashgrid_bwd_workspace_bytes(hg, B);
   const bool sorted = need != 0 && workspace && hashgrid_bwd_ws_pays(hg, B);
   if (sorted && (workspace_bytes < need || bad(workspace, 256))) return HG_ERR_INVALID_ARG;
+  const uint32_t n1 = 64 * n_in, n2 = 64 * 64, n3 = 64 * n_out;
+  if (clip && arrays_clash(hg, *st, *clip, n1 + n2 + n3, B, x, target, y, dLdy, workspace, sorted ? need : 0))
+    return HG_ERR_INVALID_ARG;
   bool counted = false;
   hg_status rc = HG_ERR_UNSUPPORTED;
   if (sorted) {
@@ -78,7 +101,6 @@ hg_status train_step(const hashgrid* hg, const hashgrid_train_state* st, uint32_
   if (rc == HG_ERR_UNSUPPORTED) rc = hashgrid_encode_fwd(hg, B, x, st->tables_half, y, stream);
   if (rc != HG_OK) return rc;
 
-  const uint32_t n1 = 64 * n_in, n2 = 64 * 64, n3 = 64 * n_out;
   const _Float16* W = static_cast<const _Float16*>(st->weights_half);
   SideJob job{};
   rc = launch_mlp_train(B, n_in, n_out, y, W, W + n1, W + n1 + n2, target, st->loss, st->loss_scale, dLdy, &job, st->scratch, s);
