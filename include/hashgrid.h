@@ -430,7 +430,8 @@ typedef struct {
  *   grad_scale  finite and positive: 1, or the reciprocal of the factor by which the loss was scaled
  *   max_norm    >= 0, infinity: no clipping, the norm is only measured (and step set)
  * A tensor that stands in the list twice counts twice.  n_tensors == 0, or tensors without scalars: the norm is 0, factor 1.
- * HG_ERR_INVALID_ARG for NULL or misaligned pointers, an unknown dtype, scales out of range. */
+ * HG_ERR_INVALID_ARG for NULL or misaligned pointers, an unknown dtype, scales out of range, and (here as below) where an array of
+ * the call shares memory with *stats. */
 hg_status hashgrid_grad_norm(uint32_t n_tensors, const hashgrid_grad* grads, float grad_scale, float max_norm,
                              hashgrid_grad_stats* stats, void* stream);
 

@@ -235,8 +235,12 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
     if (hg::misaligned(t.params_master, 4) || hg::misaligned(t.m, 4) || hg::misaligned(t.v, 4) ||
         hg::misaligned(t.grad, hg::dtype_bytes(t.grad_dtype)) || (t.params_half && hg::misaligned(t.params_half, 2)))
       return HG_ERR_INVALID_ARG;
+    const uint64_t size = t.n_scalars * hg::dtype_bytes(t.grad_dtype), four = 4 * t.n_scalars;
+    if (hg::in_stats(t.params_master, four, stats) || hg::in_stats(t.m, four, stats) || hg::in_stats(t.v, four, stats) ||
+        hg::in_stats(t.grad, size, stats) || (t.params_half && hg::in_stats(t.params_half, 2 * t.n_scalars, stats)))
+      return HG_ERR_INVALID_ARG;
     scalars += t.n_scalars;
-    bytes += t.n_scalars * hg::dtype_bytes(t.grad_dtype);
+    bytes += size;
   }
   if (scalars > HG_MAX_TENSOR_SCALARS) return HG_ERR_UNSUPPORTED;
   if (scalars == 0 && !stats) return HG_OK;

@@ -13,6 +13,11 @@ struct Range {
   uintptr_t begin, end;
   bool written;
 };
+// Whether an array shares memory with *stats, which the calls on lists write.
+inline bool in_stats(const void* array, uint64_t bytes, const hashgrid_grad_stats* stats) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(array), st = reinterpret_cast<uintptr_t>(stats);
+  return stats && bytes && at < st + sizeof(*stats) && st < at + bytes;
+}
 // Whether something is written that another array of the call shares: range_of(k, i) for k < KINDS kinds of arrays (values, gradients,
 // ...) of n <= HG_MAX_TENSORS tensors.  Each kind in the order of its addresses, as the arrays mostly come, and then all kinds
 // side by side; 2 KB of stack a kind.

@@ -242,7 +242,10 @@ hg_status check_grads(uint32_t n, const hashgrid_grad* grads, float grad_scale, 
     *scalars += grads[i].n_scalars;
     *bytes += grads[i].n_scalars * dtype_bytes(grads[i].dtype);
   }
-  return *scalars > HG_MAX_TENSOR_SCALARS ? HG_ERR_UNSUPPORTED : HG_OK;
+  if (*scalars > HG_MAX_TENSOR_SCALARS) return HG_ERR_UNSUPPORTED;
+  for (uint32_t i = 0; i < n; ++i)
+    if (in_stats(grads[i].data, grads[i].n_scalars * dtype_bytes(grads[i].dtype), stats)) return HG_ERR_INVALID_ARG;
+  return HG_OK;
 }
 
 // The next descriptions of the list from tensor i on, as many as List holds.
@@ -306,7 +309,9 @@ extern "C" hg_status hashgrid_clip_grads(uint32_t n_tensors, const hashgrid_grad
   const hg_status ok = hg::check_grads(n_tensors, grads, grad_scale, max_norm, stats, &scalars, &bytes);
   if (ok != HG_OK) return ok;
   for (uint32_t i = 0; out && i < n_tensors; ++i)
-    if (grads[i].n_scalars && hg::bad_array(out[i], grads[i].dtype)) return HG_ERR_INVALID_ARG;
+    if (grads[i].n_scalars && (hg::bad_array(out[i], grads[i].dtype) ||
+                               hg::in_stats(out[i], grads[i].n_scalars * hg::dtype_bytes(grads[i].dtype), stats)))
+      return HG_ERR_INVALID_ARG;
   const bool clash = hg::ranges_clash<2>(n_tensors, [&](int kind, uint32_t i) {
     const uintptr_t size = grads[i].n_scalars * hg::dtype_bytes(grads[i].dtype);
     const uintptr_t from = reinterpret_cast<uintptr_t>(grads[i].data), to = out ? reinterpret_cast<uintptr_t>(out[i]) : from;
