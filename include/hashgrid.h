@@ -415,7 +415,7 @@ typedef struct {
 /* Device memory, 16-byte aligned, ALL ZERO before its first use; one per model.  Calls that overlap in time need one each. */
 typedef struct {
   float norm;      /* of the last hashgrid_grad_norm; NaN or infinity where a gradient is */
-  float factor;    /* min(1, max_norm / norm); 0 where the sum of the squares is not finite */
+  float factor;    /* min(1, max_norm / norm), to the nearest fp32; 0 where the sum of the squares is not finite */
   uint32_t step;   /* number of the optimiser step that is due: steps + 1, or 0 where the sum is not finite: left out */
   uint32_t steps;  /* optimiser steps taken (hashgrid_adam_steps).  A caller that resumes sets it. */
   uint32_t reserved[28];
@@ -425,7 +425,9 @@ typedef struct {
 
 /* norm = grad_scale * sqrt(sum of the squares of all scalars of all tensors) and what follows from it, into *stats.
  * Squares and sums are held in 64 bits: no gradient is too large or too small to count, and norm is within a unit in its last
- * place of the exact one (infinity beyond fp32's range; factor does not suffer from that).  The same arrays give the same bits.
+ * place of the exact one (infinity beyond fp32's range; factor comes from the one in 64 bits).  factor has all its bits where norm is
+ * at most 2^126 times max_norm; beyond that it is a subnormal, off by up to 2^-150, and the clipped norm by 2^-150 norm: of a norm
+ * of 1e41 and a bound of 1e-4 a clipped norm of 1.4e-4 comes.  From 2^150 times max_norm on it is 0.  The same arrays give the same bits.
  *   grads       [n_tensors]  HOST array, read during the call; data is read only
  *   grad_scale  finite and positive: 1, or the reciprocal of the factor by which the loss was scaled
  *   max_norm    >= 0, infinity: no clipping, the norm is only measured (and step set)
@@ -436,7 +438,8 @@ hg_status hashgrid_grad_norm(uint32_t n_tensors, const hashgrid_grad* grads, flo
                              hashgrid_grad_stats* stats, void* stream);
 
 /* hashgrid_grad_norm, and then out_i = factor * grads_i, each product rounded (nearest even) to the tensor's type from fp32 or,
- * fp16 ones, at once: the gradients keep their loss scale.  factor == 0 (max_norm 0, or a gradient that is not finite) writes zeros, which hashgrid_adam_step passes over.
+ * fp16 ones, at once: the gradients keep their loss scale.  factor == 0 (max_norm 0, a norm 2^150 times as large, or a
+ * gradient that is not finite) writes zeros, which hashgrid_adam_step passes over.
  * (hashgrid_adam_steps clips on its way and needs the norm alone.)
  *   out  [n_tensors]  HOST array of device pointers to arrays of the gradients' types and sizes; out[i] == grads[i].data
  *                     is in place.  NULL: all in place; where factor is 1 nothing is written then.
@@ -458,7 +461,8 @@ typedef struct {
 } hashgrid_adam_tensor;
 
 /* hashgrid_adam_step on every tensor of the list, in one launch for every four dozen of them.  The gradient that the step takes is
- * grad * (grad_scale * factor), in fp32, plus cfg.l2_reg * value; scalars for which that is exactly 0 are passed over.
+ * grad * (grad_scale * factor), in fp32 (the product in brackets too: below 2^-126 it has fewer bits), plus cfg.l2_reg * value;
+ * scalars for which that is exactly 0 are passed over: their moments do not decay.
  *   tensors  [n_tensors]  HOST array, read during the call
  *   stats    NULL: factor 1, and the step's number is `step` >= 1.
  *            Else `step` is 0 and both come from the last hashgrid_grad_norm on *stats: factor, and step, which becomes
