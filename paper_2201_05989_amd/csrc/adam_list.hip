@@ -5,10 +5,11 @@
 // beside its gradient; the clipped gradient is never stored.  Scalars without a gradient keep every bit, but memory is read and
 // written by the line: where one of the 32 scalars that share a line of each fp32 array has a gradient, all of the line is read
 // and written back, past the caches where they do not hold it all from one step to the next.  Left out lane by lane, the
-// stores leave lines with holes behind, which cost the memory more than whole ones (norm and step, fp32 gradients: 58 M scalars
-// of which 22 % have one 437 -> 321 us, 408 M with 63 % 2.92 -> 2.61 ms, 12 M with 95 % 85 -> 75; lines passed by the caches and left
-// out lane by lane 466, 3.80, 76).  Lines in which no scalar has a gradient cost their gradient's bytes.
-// (Step alone: 408 M scalars 2.3 ms, 12.2 GB in whole lines at 5.3 TB/s, where a large copy reaches 4.9; 12 M 62 us.)
+// stores leave lines with holes behind, which cost the memory more than whole ones (norm and step, fp32 gradients, three models in
+// turn, whole lines and lane by lane: 58 M scalars of which 22 % have one 308 and 462 us, 408 M with 63 % 2.56 and 3.76 ms, 12 M with
+// 95 % 73.6 and 74.3 us; 4, 16 or 64 lanes together instead of a line's eight: 310 to 311 us, 2.54 to 2.55 ms, 73.3 to 73.5 us).
+// Lines in which no scalar has a gradient cost their gradient's bytes.
+// (Step alone: 408 M scalars 2.3 ms, 12.2 GB in whole lines at 5.3 TB/s, where a large copy reaches 4.9; 12 M 63 us.)
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -97,9 +98,10 @@ __device__ __forceinline__ void store_copy(void* array, const uint32_t dtype, co
 }
 
 // Which arrays are read past the caches.  kState: values and moments, where a step's arrays are more than kResidentBytes: beyond
-// that they do not survive until the next step (norm and step, three models in turn, of 4.5 M scalars, 81 MB each, 34.1 us past
-// the caches and 30.5 through them; 6 M, 108 MB, 41.5 and 41.9; 14 M, 252 MB, 83.7 and 93.7.  One model of 12 M, 220 MB, and
-// nothing else running, 75 and 71: in a training step, whose other passes need the caches, the same).
+// that they do not survive until the next step (norm and step, three models in turn, of 4.5 M scalars, 81 MB each, 33.4 us past
+// the caches and 29.9 through them; 6 M, 108 MB, 40.5 and 40.8; 12 M, 220 MB, 73.6 and 82.5; 14 M, 252 MB, 83.2 and 94.0.  One model of
+// 12 M with nothing else running 73.3 and 71.2; in a clipped training step of 2^18 points, whose other passes need the caches, 317
+// both ways, and with 58 M scalars 550 and 597).
 // kAll: the gradients as well, where the norm has read them past the caches (kCacheBytes).
 enum class Reach { kNone, kState, kAll };
 constexpr uint64_t kResidentBytes = 96u << 20;
@@ -112,7 +114,7 @@ __device__ __forceinline__ void step_span(const AdamItem& it, const AdamArgs& a,
   void* const copy = it.st.p16;
   float *const p = it.st.p32, *const m = it.st.m, *const v = it.st.v;
   const uint32_t n = (uint32_t)(end - begin), n4 = n / 4, gt = it.at.dtype, ct = it.at.copy_dtype;
-  // (two or eight vectors ahead instead of four: 78 and 79 us for 75 on 12 M scalars, norm included)
+  // (two or eight vectors ahead instead of four: 74.2 and 76.5 us for 73.6 on 12 M scalars, norm included)
   for_vectors<4, kListThreads>(n4, threadIdx.x, [&](const uint32_t q0, auto many) __attribute__((always_inline)) {
     constexpr int K = decltype(many)::value;
     Bits4 bits[K];
@@ -256,7 +258,7 @@ extern "C" hg_status hashgrid_adam_steps(uint32_t n_tensors, const hashgrid_adam
   const uint64_t all = bytes + 14 * scalars;  // with value, moments and copy
   const hg::Reach reach = bytes > hg::kCacheBytes ? hg::Reach::kAll : all > hg::kResidentBytes ? hg::Reach::kState : hg::Reach::kNone;
   // Half as many workgroups where that still leaves each some ten units: with fewer streams open the memory is faster (norm and
-  // step on 58 M scalars 305 us with 512 and 320 with 1024, on 12 M 74.3 and 73.5, on 7 M 48.7 and 46.5).
+  // step on 58 M scalars 308 us with 512 and 321 with 1024, on 12 M 74.8 and 73.6, on 7 M 46.6 and 45.9).
   const uint32_t most = scalars > (32u << 20) ? hg::kMaxListGroups / 2 : hg::kMaxListGroups;
   hg::AdamList list;
   list.unit = hg::step_unit_for(scalars);

@@ -7,10 +7,10 @@
 // where losses are means), and a sum of 2^29 of them would lose some more; 64-bit multiply-adds run at the rate of the 32-bit
 // ones here, two instructions a scalar beside 4 bytes of memory traffic.  Every workgroup leaves its sum in an array and the
 // last one adds those up in the order of their places: the norm of the same arrays is the same bits every time.
-// (408 M scalars: fp16 122 us, 6.7 TB/s; fp32 250 us, 6.5 TB/s, where a large copy reaches 4.9.  12 M fp32 scalars
-// 12.5 us, of which 4 are the launch, the first loads and the meeting of the workgroups at the end.)
+// (408 M scalars: fp16 121 us, 6.7 TB/s; fp32 236 us, 6.9 TB/s, where a large copy reaches 4.9.  12 M fp32 scalars
+// 11.7 us, of which 4 are the launch, the first loads and the meeting of the workgroups at the end.)
 //
-// Clipping reads and writes what it cannot be spared once more (58 M fp16 scalars into other arrays: 24 us for the norm
+// Clipping reads and writes what it cannot be spared once more (58 M fp16 scalars into other arrays: 54.8 us, 23 for the norm
 // and 32, 7.3 TB/s, the second reading from the last-level cache), and nothing where the factor is 1 and it is in place.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -130,8 +130,8 @@ __global__ __launch_bounds__(kListThreads) void norm(const NormList list, hashgr
     if (groups > 1) {
       // The sum is performed before this workgroup is counted: it, the counters and the last one's loads are device-scope
       // atomics, which meet behind the caches, so nothing else has to be ordered.  (With release and acquire on the
-      // counter, which write this XCD's L2 back, the norm of 12 M scalars took 42 us for 15, 408 M fp16 243 for 145; a launch
-      // of its own for the last sums 9.1 us for 5.9 on 6 K scalars, caller's time included.)
+      // counter, which write this XCD's L2 back, the norm of 12 M scalars takes 35 us for 11.7, 408 M fp16 160 for 121; with a
+      // launch of their own for the last sums 13.1 and 123, and 4.5 M scalars 9.1 for 7.9.)
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       last = last_to_arrive(st->arrived);
     }
@@ -194,8 +194,9 @@ __global__ __launch_bounds__(kListThreads) void clip(const ClipList list, const 
 }
 
 // Norm, and clipping where `clipped`, of a list that one workgroup is enough for: its sixteen waves are the teams, with a unit each at
-// the most.  (Norm of 3 K scalars in three tensors 2.6 us, in several workgroups 4.2; clipped 3.8, in two launches 6.0; 32 K scalars
-// 3.5 and 4.6, 6.4 and 6.4; 32 tensors of 100, two units a wave, 5.1 and 4.8, 8.7 and 6.7.  GPU time of calls one after the other.)
+// the most.  (Norm of 3 K scalars in three tensors 2.7 us, in several workgroups 4.3; clipped 3.8, in two launches 6.7.  With two units
+// a wave 32 K scalars would take 4.4 us for the 4.5 of several workgroups, clipped 6.9 for 6.8, and 32 tensors of 100 3.5 for 4.5, clipped
+// 5.5 for 7.0, which this rule gives away.  GPU time of calls one after the other, in a graph.)
 constexpr int kSmallThreads = 1024;
 __global__ __launch_bounds__(kSmallThreads) void small_list(const ClipList list, hashgrid_grad_stats* __restrict__ st, const bool clipped,
                                                             const float grad_scale, const float max_norm) {

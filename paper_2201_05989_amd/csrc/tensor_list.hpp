@@ -4,8 +4,8 @@
 // The arrays' descriptions travel by value in the kernel's arguments, so that a call neither copies nor allocates device
 // memory and can be recorded into a graph.  The arrays are cut into units of some thousand scalars, numbered through all arrays of
 // the list, and dealt out to the workgroups in turn: arrays of any sizes, one scalar or 2^32 and more, give workgroups the same
-// work to within a unit, and what the chip reads at a time lies together (in turn 2.94 ms, a run of its own for each workgroup
-// 2.99: norm and optimiser step on 408 M fp32 scalars, before the other steps that the kernels name).  Scalars are read and
+// work to within a unit, and what the chip reads at a time lies together (in turn 2.56 ms, a run of its own for each workgroup
+// 2.64: norm and optimiser step on 408 M fp32 scalars; on 12 M 73.6 and 76.7 us).  Scalars are read and
 // written 16 bytes a lane wherever the array starts: global loads and stores of this target need no more than the
 // element's own alignment.
 #pragma once
@@ -24,8 +24,8 @@ constexpr int kListThreads = 256;
 constexpr uint32_t kSmallUnit = 2048, kLargeUnit = 8192;
 constexpr uint32_t kWaveUnit = 1024;  // where a team is one wave: 16 a lane
 // Workgroups at most, four a compute unit: as many as run at a time in the optimiser step, whose four vectors ahead take the
-// registers.  Norm and clipping, of which more fit, read no faster with more (norm of 408 M fp16 scalars 122 us with 1024 and 129
-// with 2048, of 12 M fp32 13.5 and 14.1).
+// registers.  Norm and clipping, of which more fit, read no faster with more (norm of 408 M fp16 scalars 121 us with 1024 and 128
+// with 2048, of 12 M fp32 11.7 and 12.9).
 constexpr uint32_t kMaxListGroups = 1024;
 
 // What every description of an array begins its place in the list with: its first unit, and the scalars of its last one (the
@@ -96,20 +96,20 @@ Place next_place(List& list, uint64_t n, uint32_t dtype, uint32_t copy_dtype = 0
 }
 
 // Scalars a unit for a list of so many.  Norm and clipping: the smallest unit with which a workgroup has two at the most, and the
-// large one beyond that (4.5 M fp32 scalars: norm 8.6 us with units of 4096 and 10.6 with 2048, clipped 13.2 and 15.1;
-// 12 M 14.8 with 8192, 16.3 with 6144 and 17.2 with 2048; 408 M fp16 145 with 8192 and 183 with 2048).
+// large one beyond that (4.5 M fp32 scalars: norm 7.8 us with units of 4096 as with 2048, clipped 12.6 and 12.5; 12 M 11.7 with 8192,
+// 12.0 with 4096 and 12.1 with 2048; 408 M fp16 121 with 8192, 120 with 4096 and 187 with 2048).
 inline uint32_t unit_for(uint64_t scalars) {
   uint32_t unit = kSmallUnit;
   while (unit < kLargeUnit && scalars > 2ull * unit * kMaxListGroups) unit *= 2;
   return unit;
 }
-// The optimiser step, with four arrays to a scalar, fills the memory with small units for longer (norm and step on 6 M scalars 41.6
-// us with 2048 and 43.3 with 4096, 408 M 2.94 ms with 8192 and 3.2 with 2048).
+// The optimiser step, with four arrays to a scalar, fills the memory with small units for longer (norm and step on 6 M scalars 40.8
+// us with 2048, 40.9 with 4096 and 42.7 with 8192; 12 M 72.8, 74.2 and 73.4; 408 M between 2.53 and 2.56 ms with each).
 inline uint32_t step_unit_for(uint64_t scalars) { return scalars > (8u << 20) ? kLargeUnit : kSmallUnit; }
 
 // Whether a list's gradients are too many for the last-level cache to hold from the norm's reading to the next: both then
-// pass by the caches.  (Measured on either side: norm and optimiser step on 408 M fp32 gradients, 1.6 GB, 2.57 ms passing by and
-// 2.61 through the caches, the norm of as many fp16 ones 130 us and 145; on 58 M fp32, 232 MB, 353 and 320, on 12 M 81 and 75.)
+// pass by the caches.  (Measured on either side: the norm of 408 M fp16 gradients 121 us passing by and 135 through the caches, fp32,
+// 1.6 GB, 236 and 266; norm and optimiser step on the latter 2.56 ms and 2.53; on 58 M fp32, 232 MB, 342 us and 308, on 12 M 79 and 73.6.)
 constexpr uint64_t kCacheBytes = 256u << 20;
 
 inline uint32_t groups_of(uint32_t units, uint32_t most = kMaxListGroups) { return units < most ? (units ? units : 1) : most; }
@@ -133,7 +133,8 @@ __device__ __forceinline__ Vec<T, V> load_vec(const T* p) {
   else
     return __builtin_bit_cast(Vec<T, V>, *at);
 }
-// Every store here is of that kind (clipping 58 M fp16 scalars into other arrays 75 -> 63 us, norm and step on 408 M 3.46 -> 3.00 ms).
+// Every store here is of that kind (clipping 58 M fp16 scalars into other arrays 54.8 us, with plain stores 77.3; norm and step on 408 M
+// 2.56 ms and 2.71, on 12 M 73.6 us and 79.7).
 template <typename T, int V>
 __device__ __forceinline__ void store_vec(T* p, const Vec<T, V>& v) {
   __builtin_nontemporal_store(__builtin_bit_cast(typename VecOf<T, V>::type, v), reinterpret_cast<typename VecOf<T, V>::type*>(p));
