@@ -56,19 +56,19 @@ __device__ __forceinline__ Bits4 load_bits(const void* array, const uint32_t dty
   if (dtype == HG_F32) {
     b = __builtin_bit_cast(Bits4, load_vec<float, 4, STREAM>(static_cast<const float*>(array) + at));
   } else {
-    const Vec<uint16_t, 4> h = load_vec<uint16_t, 4, STREAM>(static_cast<const uint16_t*>(array) + at);
+    const Scalars<uint16_t, 4> h = load_vec<uint16_t, 4, STREAM>(static_cast<const uint16_t*>(array) + at);
     const uint2 two = __builtin_bit_cast(uint2, h);
     b.w[0] = two.x;
     b.w[1] = two.y;
   }
   return b;
 }
-__device__ __forceinline__ Vec<float, 4> to_floats(const Bits4& b, const uint32_t dtype) {
-  Vec<float, 4> f;
+__device__ __forceinline__ Scalars<float, 4> to_floats(const Bits4& b, const uint32_t dtype) {
+  Scalars<float, 4> f;
   if (dtype == HG_F32) {
     f = __builtin_bit_cast(decltype(f), b);
   } else if (dtype == HG_F16) {
-    const Vec<_Float16, 4> h = __builtin_bit_cast(decltype(h), make_uint2(b.w[0], b.w[1]));
+    const Scalars<_Float16, 4> h = __builtin_bit_cast(decltype(h), make_uint2(b.w[0], b.w[1]));
 #pragma unroll
     for (int j = 0; j < 4; ++j) f.v[j] = (float)h.v[j];
   } else {  // bf16: the upper half of a float
@@ -79,18 +79,18 @@ __device__ __forceinline__ Vec<float, 4> to_floats(const Bits4& b, const uint32_
 }
 __device__ __forceinline__ void store_zeros(void* array, const uint32_t dtype, const uint64_t at) {
   if (dtype == HG_F32)
-    store_vec<float, 4>(static_cast<float*>(array) + at, Vec<float, 4>{});
+    store_vec<float, 4>(static_cast<float*>(array) + at, Scalars<float, 4>{});
   else
-    store_vec<uint16_t, 4>(static_cast<uint16_t*>(array) + at, Vec<uint16_t, 4>{});
+    store_vec<uint16_t, 4>(static_cast<uint16_t*>(array) + at, Scalars<uint16_t, 4>{});
 }
-__device__ __forceinline__ void store_copy(void* array, const uint32_t dtype, const uint64_t at, const Vec<float, 4>& p) {
+__device__ __forceinline__ void store_copy(void* array, const uint32_t dtype, const uint64_t at, const Scalars<float, 4>& p) {
   if (dtype == HG_F16) {
-    Vec<_Float16, 4> h;
+    Scalars<_Float16, 4> h;
 #pragma unroll
     for (int j = 0; j < 4; ++j) h.v[j] = (_Float16)p.v[j];
     store_vec<_Float16, 4>(static_cast<_Float16*>(array) + at, h);
   } else {
-    Vec<__bf16, 4> h;
+    Scalars<__bf16, 4> h;
 #pragma unroll
     for (int j = 0; j < 4; ++j) h.v[j] = (__bf16)p.v[j];
     store_vec<__bf16, 4>(static_cast<__bf16*>(array) + at, h);
@@ -118,7 +118,7 @@ __device__ __forceinline__ void step_span(const AdamItem& it, const AdamArgs& a,
   for_vectors<4, kListThreads>(n4, threadIdx.x, [&](const uint32_t q0, auto many) __attribute__((always_inline)) {
     constexpr int K = decltype(many)::value;
     Bits4 bits[K];
-    Vec<float, 4> g[K], pp[K], mm[K], vv[K];
+    Scalars<float, 4> g[K], pp[K], mm[K], vv[K];
     bool any[K], run[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) bits[k] = load_bits<REACH == Reach::kAll>(grad, gt, begin + (q0 + k * kListThreads) * 4);

@@ -47,7 +47,7 @@ __device__ __forceinline__ double sum_squares(const T* __restrict__ g, const uin
   double sum[2] = {0.0, 0.0};
   for_vectors<4, THREADS>(n_vec, thread, [&](const uint32_t q, auto many) __attribute__((always_inline)) {
     constexpr int K = decltype(many)::value;
-    Vec<T, V> x[K];
+    Scalars<T, V> x[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) x[k] = load_vec<T, V, STREAM>(base + (q + k * THREADS) * V);
 #pragma unroll
@@ -167,7 +167,7 @@ __device__ __forceinline__ void scale_span(const T* g, T* out, const float facto
   auto scaled = [&](const T x) { return factor == 0.0f ? (T)0.0f : (T)((float)x * factor); };
   for_vectors<4, THREADS>(n_vec, thread, [&](const uint32_t q, auto many) __attribute__((always_inline)) {
     constexpr int K = decltype(many)::value;
-    Vec<T, V> x[K];
+    Scalars<T, V> x[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) x[k] = load_vec<T, V, true>(from + (q + k * THREADS) * V);
 #pragma unroll
