@@ -440,7 +440,7 @@ hg_status hashgrid_grad_norm(uint32_t n_tensors, const hashgrid_grad* grads, flo
 /* hashgrid_grad_norm, and then out_i = factor * grads_i, each product rounded (nearest even) to the tensor's type from fp32 or,
  * fp16 ones, at once: the gradients keep their loss scale.  factor == 0 (max_norm 0, a norm 2^150 times as large, or a
  * gradient that is not finite) writes zeros, which hashgrid_adam_step passes over.
- * (hashgrid_adam_steps clips on its way and needs the norm alone.)
+ * (hashgrid_adam_steps clips on its way and needs the norm alone: after clipping in place it would take the factor a second time.)
  *   out  [n_tensors]  HOST array of device pointers to arrays of the gradients' types and sizes; out[i] == grads[i].data
  *                     is in place.  NULL: all in place; where factor is 1 nothing is written then.
  * HG_ERR_INVALID_ARG also where an array that is written shares memory with another one of the call. */

@@ -571,7 +571,8 @@ def grad_norm(grads, stats: GradStats, max_norm: float = math.inf, grad_scale: f
 def clip_grads(grads, max_norm: float, stats: GradStats, out=None, grad_scale: float = 1.0, stream=None) -> torch.Tensor:
     """hashgrid_clip_grads: grad_norm, and the gradients times stats.factor, in place or into the tensors of `out` (of the same
     types and sizes); gradients that are not all finite become zeros.  They keep their loss scale.  Returns stats.norm, as
-    it was before.  (adam_steps clips on its way and needs grad_norm alone.)"""
+    it was before.  (adam_steps clips on its way and needs grad_norm alone: after clipping in place it would take the factor a
+    second time.)"""
     g = _grad_list(grads)
     to = None if out is None else _grad_list(out)
     if to is not None and (to._kinds != g._kinds or to._device != g._device):
@@ -587,7 +588,8 @@ _stamps = itertools.count(1)
 @dataclass(eq=False)
 class AdamTensor:
     """One tensor of adam_steps: fp32 master copy and moments, gradient (fp32, fp16 or bf16), 16-bit working copy or None, and
-    the hyper-parameters.  Any of them may be replaced between steps."""
+    the hyper-parameters.  Any of them may be replaced between steps.  Scalars whose gradient is exactly 0 are passed over: without
+    an L2 term neither they nor their moments change."""
     params_master: torch.Tensor
     grad: torch.Tensor
     m: torch.Tensor
