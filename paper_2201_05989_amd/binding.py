@@ -555,14 +555,19 @@ class GradList:
         return len(self.tensors)
 
 
-def _grad_list(grads) -> GradList:
-    return grads._current() if isinstance(grads, GradList) else GradList(grads)._current()
+def _current_list(kind, tensors):
+    """A list of that kind as it is now: a kept one looked over again, one of these tensors made."""
+    if isinstance(tensors, kind):
+        return tensors._current()
+    made = kind(tensors)
+    _on_current_device(made._device, "tensors")
+    return made
 
 
 def grad_norm(grads, stats: GradStats, max_norm: float = math.inf, grad_scale: float = 1.0, stream=None) -> torch.Tensor:
     """hashgrid_grad_norm over a GradList or any sequence of tensors: returns stats.norm, grad_scale times the Euclidean
     norm of all scalars; stats.factor is what brings it down to max_norm."""
-    g = _grad_list(grads)
+    g = _current_list(GradList, grads)
     _check(load_library().hashgrid_grad_norm(len(g), g._array, grad_scale, max_norm, _stats_ptr(stats), _stream_ptr(stream)),
            "hashgrid_grad_norm")
     return stats.norm
@@ -573,8 +578,8 @@ def clip_grads(grads, max_norm: float, stats: GradStats, out=None, grad_scale: f
     types and sizes); gradients that are not all finite become zeros.  They keep their loss scale.  Returns stats.norm, as
     it was before.  (adam_steps clips on its way and needs grad_norm alone: after clipping in place it would take the factor a
     second time.)"""
-    g = _grad_list(grads)
-    to = None if out is None else _grad_list(out)
+    g = _current_list(GradList, grads)
+    to = None if out is None else _current_list(GradList, out)
     if to is not None and (to._kinds != g._kinds or to._device != g._device):
         raise HashGridError("out must be tensors of the gradients' types and sizes, on their device")
     _check(load_library().hashgrid_clip_grads(len(g), g._array, None if to is None else to._pointers, grad_scale, max_norm,
@@ -663,7 +668,7 @@ def adam_steps(tensors, stats: GradStats | None = None, step: int = 0, zero_grad
     """hashgrid_adam_steps on an AdamList or any sequence of AdamTensor: adam_step on all of them in one launch.  With
     stats, after grad_norm over the same gradients: they are clipped on the way, the step is left out where one of them is not
     finite, and the device counts the steps.  Without: the step's number is `step`, counted from 1."""
-    a = tensors._current() if isinstance(tensors, AdamList) else AdamList(tensors)._current()
+    a = _current_list(AdamList, tensors)
     _check(load_library().hashgrid_adam_steps(len(a), a._array, grad_scale, int(zero_grad), step,
                                               None if stats is None else _stats_ptr(stats), _stream_ptr(stream)),
            "hashgrid_adam_steps")
