@@ -236,6 +236,7 @@ class HashGrid:
         self.n_entries = int(self._lib.hashgrid_n_entries(self._h))
         self._batch = (0, False, 0)  # the last batch size asked about: (B, bwd_ws_pays, bwd_workspace_bytes)
         self._ws = {}  # (device, stream) -> scratch buffer kept for calls that pass none
+        self._recorded = {}  # address -> such a buffer that a captured call uses: kept for the replays
         self._counted = None  # (x pointer, B, workspace pointer, x version, stream) the workspace holds counts for
 
     def __del__(self):
@@ -262,6 +263,8 @@ class HashGrid:
             self._ws[key] = ws
         if stream is not None:
             ws.record_stream(stream)  # allocated on torch's current stream, used on this one
+        if torch.cuda.is_current_stream_capturing():
+            self._recorded[ws.data_ptr()] = ws  # a graph's from here on, also where this object goes on with a larger one
         return ws
 
     def _of_batch(self, B: int):

@@ -54,7 +54,7 @@ class HashGridModel:
             n_out=n_out, tables_adam=hashgrid_adam_config(0.0, 0.9, 0.99, 1e-15, 0.0),
             weights_adam=hashgrid_adam_config(0.0, 0.9, 0.99, 1e-15, 0.0), loss_sum=self._loss_sum.data_ptr(),
             scratch=self._scratch.data_ptr())
-        self._buf_B = 0
+        self._buf_B, self._recorded = 0, {}
         self._max_grad_norm = self._grads = None
         self.max_grad_norm = max_grad_norm
 
@@ -102,9 +102,14 @@ class HashGridModel:
 
     def _buffers(self, B: int):
         if B != self._buf_B:
-            self._y = torch.empty((B, self.n_in), dtype=torch.float16, device="cuda")
-            self._dy = torch.empty_like(self._y)
+            if B in self._recorded:
+                self._y, self._dy = self._recorded[B]
+            else:
+                self._y = torch.empty((B, self.n_in), dtype=torch.float16, device="cuda")
+                self._dy = torch.empty_like(self._y)
             self._buf_B = B
+        if torch.cuda.is_current_stream_capturing():  # the graph's from here on: kept for its replays when other batches come
+            self._recorded[B] = self._y, self._dy
 
     def _network(self):
         """W1, W2, W3 of weights_half as it is now.  The views are made again where it lies elsewhere than they do (they keep
